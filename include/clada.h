@@ -417,6 +417,101 @@ clada_status clada_static_ffn_decode(clada_ctx *ctx, const clada_layer *layer, c
                                      int32_t B, const int32_t *active_idx, const int32_t *n_active,
                                      void *y, void *hip_stream);
 
+/* ---- Attention beside the FFN calls: a key / value cache, the rotation that fills it, and the attention that reads it.
+ *
+ * clada_heads: a view [B][T][H][d] of queries, keys, values or outputs; strides in elements, the d values of a head
+ * contiguous.  clada_kv_cache: keys and values [batch][heads][capacity][d] of one shape and one set of strides.  Pointers and
+ * strides are multiples of 16 bytes, strides are not negative (an input may have strides of 0); d is a multiple of 8.
+ * Without a ring (ring = 0) row n of a cache holds the token at position n.  With one, positions below n_sink have their own
+ * rows and a later position p lies in row n_sink + (p - n_sink) % ring, where it replaces position p - ring.  Keys are
+ * stored rotated, so attention does not mind the order of rows. */
+#define CLADA_ATTN_MAX_D 256       /* values of a head                        */
+#define CLADA_ATTN_MAX_HEADS 1024  /* query heads                             */
+#define CLADA_ATTN_MAX_BATCH 4096  /* sequences of a call                     */
+#define CLADA_ATTN_MAX_ROWS (1 << 20) /* B * T of a call                      */
+
+typedef struct {
+    void *data;
+    int64_t stride_b, stride_t, stride_h;
+} clada_heads;
+
+typedef struct {
+    void *k, *v;
+    int64_t stride_b, stride_h, stride_n;   /* elements: sequence, head, row; the same for k and v */
+    int32_t batch, heads, d, capacity;
+    int32_t dtype;                          /* a clada_dtype; queries and outputs have it too */
+    int32_t n_sink, ring;
+} clada_kv_cache;
+
+/* Rotary positions.  Pair i of a head turns by the angle position * f_i.  CLADA_ROPE_HALF pairs values i and i + rotary_dim/2,
+ * CLADA_ROPE_PAIRS values 2i and 2i + 1; values from rotary_dim on are left alone.  `turns` (device, [rotary_dim/2]) holds f_i as
+ * 2^64ths of a turn, which wraps exactly at any position; cosines and sines are multiplied by `magnitude`. */
+typedef enum { CLADA_ROPE_HALF = 0, CLADA_ROPE_PAIRS = 1 } clada_rope_layout;
+typedef struct {
+    const uint64_t *turns;
+    int32_t rotary_dim;                     /* R, even, 0 (no rotation) to d */
+    int32_t layout;
+    float magnitude;
+} clada_rope;
+
+/* Frequencies f_i = theta^(-2i/R) and their scalings for contexts longer than `original_len` by `factor`:
+ *   NONE    as they are                    LINEAR  f_i / factor
+ *   BASE    theta * factor^(R/(R-2)) in place of theta
+ *   BANDS   f_i where a wave fits original_len at least `high` times, f_i / factor where at most `low` times, linear in that
+ *           count between
+ *   RAMP    the same two ends, blended linearly over the pair's index from floor(i(high)) to ceil(i(low)),
+ *           i(n) = R ln(original_len / (2 pi n)) / (2 ln theta); magnitude = 0.1 ln(factor) + 1 (all others: 1)
+ * clada_rope_turns fills host memory: turns [R/2] and *magnitude.  It touches no GPU; the caller copies the turns to the device. */
+typedef enum { CLADA_ROPE_SCALE_NONE = 0, CLADA_ROPE_SCALE_LINEAR = 1, CLADA_ROPE_SCALE_BASE = 2, CLADA_ROPE_SCALE_BANDS = 3,
+               CLADA_ROPE_SCALE_RAMP = 4 } clada_rope_scale;
+typedef struct {
+    double theta, factor, original_len, low, high;
+    int32_t kind;
+} clada_rope_scaling;
+clada_status clada_rope_turns(clada_ctx *ctx, int32_t rotary_dim, const clada_rope_scaling *scaling, uint64_t *turns, float *magnitude);
+
+/* Norms of queries and keys for each head: x / sqrt(mean(x^2) + eps) * (weight + offset), ahead of the rotation; weights [d] in
+ * the cache's dtype, NULL for no factor (offset then plays no part). */
+typedef struct {
+    const void *q_weight, *k_weight;
+    float eps, offset;
+} clada_head_norm;
+
+/* One pass over the projections of B sequences of T tokens: norm (NULL: none) and rotation of q [B][T][Hq][d] into q_out (which may
+ * be q), the same of k [B][T][heads][d] into the cache, v into the cache as it is.  positions [B][T] (device): a negative one marks
+ * padding, whose query is zeros and which stores nothing.  slots [B][T] (device) names the cache row of every token, negative or
+ * past the capacity: not stored; NULL: by the position, as above (a position past the capacity is not stored; with a ring
+ * T <= ring).  The rows that a call stores into must be distinct.  q and q_out, or k and v, may be NULL: keys or queries alone.
+ * All arithmetic in fp32, one rounding at the end. */
+clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, const clada_head_norm *norm, int32_t B, int32_t T, int32_t Hq,
+                           const clada_heads *q, const clada_heads *k, const clada_heads *v, const int32_t *positions,
+                           const int32_t *slots, const clada_heads *q_out, const clada_kv_cache *cache, void *hip_stream);
+
+/* Upper bound of the workspace the two attention calls make use of (beside clada_workspace_bytes: a context for both needs the
+ * larger of the two). */
+size_t clada_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t d);
+
+/* Causal attention with a sliding window and sinks.  lens [B] (device): tokens that sequence b holds, the call's own among them
+ * (those must be in the cache already); q_lens [B] (device) or NULL (T each): queries of sequence b, the first q_lens[b] rows of
+ * q [B][T][Hq][d].  Query t has position pos = lens[b] - q_lens[b] + t and sees the positions p <= pos with
+ *   window = 0, or p > pos - window, or p < sinks.
+ * out [B][T][Hq][d] = sum_p softmax_p(scale q . k_p) v_p; lse [B][T][Hq] fp32 (or NULL) = log sum_p exp(scale q . k_p).
+ * Query head h reads key head h / (Hq / heads).  A query that sees nothing (a row past q_lens[b], a negative position) gives zeros
+ * and an lse of -inf.  T = 1 is a decode step, T = lens a prompt.  Without a ring lens[b] <= capacity (more is taken as capacity);
+ * with one, window >= 1, ring >= window + T - 1 and sinks <= n_sink.  Cache rows that a query does not see do not reach its output,
+ * whatever they hold.  Scores, sums and outputs are accumulated in fp32.  Bit-reproducible from run to run. */
+clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada_kv_cache *cache, const int32_t *lens,
+                               const int32_t *q_lens, int32_t B, int32_t T, int32_t Hq, int32_t window, int32_t sinks, float scale,
+                               const clada_heads *out, float *lse, void *hip_stream);
+
+/* A decode step of B sequences behind one prefix: query b (q [B][1][Hq][d]) sees the first prefix_len rows of `prefix` (a cache of one
+ * sequence, batch >= 1, read at sequence 0) and the first lens[b] (device; 0 allowed, more than the capacity is taken as the
+ * capacity) rows of its own in `cache`.  The prefix is read for all sequences at once.  out [B][1][Hq][d] and lse [B][Hq] as above.
+ * Neither cache has a ring; both have one dtype, head count and d. */
+clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, const clada_kv_cache *prefix, int32_t prefix_len,
+                                      const clada_kv_cache *cache, const int32_t *lens, int32_t B, int32_t Hq, float scale,
+                                      const clada_heads *out, float *lse, void *hip_stream);
+
 /* One decode step as a replayable HIP graph (the algorithm "CLADA Inference", generation
  * phase, is the same short sequence of calls for every token: signals, thresholds, one
  * sparse FFN per layer; captured once, a replay costs one launch instead of 2 L + 2).

@@ -14,4 +14,7 @@ from .binding import (Context, Layer, PrefixStats, CladaError, cognitive_signals
                       mask_sparse_encode, mask_sparse_decode, mask_sparse_encode_batch,
                       mask_sparse_decode_batch, sparse_ffn_stack_decode,
                       dense_ffn_stack_decode, layer_array,
-                      workspace_bytes, Graph, graph_begin, graph_end)
+                      workspace_bytes, Graph, graph_begin, graph_end,
+                      KVCache, RopePlan, rope_plan, qk_rope, window_attn, shared_prefix_attn,
+                      attn_workspace_bytes, ROPE_HALF, ROPE_PAIRS, ROPE_SCALE_NONE, ROPE_SCALE_LINEAR,
+                      ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP)

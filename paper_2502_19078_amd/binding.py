@@ -41,6 +41,32 @@ class _CPrefixOut(C.Structure):
                 ("sum_abs_act", "sum_sq_act", "max_abs_act", "sum_sq_h", "A", "abs_act_pool")]
 
 
+class _CHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class _CKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_n", C.c_int64),
+                ("batch", C.c_int32), ("heads", C.c_int32), ("d", C.c_int32), ("capacity", C.c_int32), ("dtype", C.c_int32),
+                ("n_sink", C.c_int32), ("ring", C.c_int32)]
+
+
+ROPE_HALF, ROPE_PAIRS = 0, 1       # clada_rope_layout
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP = range(5)      # clada_rope_scale
+
+
+class _CRope(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float)]
+
+
+class _CRopeScaling(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("theta", "factor", "original_len", "low", "high")] + [("kind", C.c_int32)]
+
+
+class _CHeadNorm(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("offset", C.c_float)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -104,11 +130,17 @@ def load_library() -> C.CDLL:
     lib.clada_graph_destroy.argtypes = [vp]
     lib.clada_graph_destroy.restype = None
     lib.clada_diag_kernel_times.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float)]
+    lib.clada_rope_turns.argtypes = [vp, i32, C.POINTER(_CRopeScaling), vp, C.POINTER(C.c_float)]
+    lib.clada_qk_rope.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.clada_window_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]
+    lib.clada_shared_prefix_attn.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, f32, vp, vp, vp]
+    lib.clada_attn_workspace_bytes.argtypes = [i32] * 4
+    lib.clada_attn_workspace_bytes.restype = C.c_size_t
     for name in ("clada_diag_stream_read", "clada_diag_copy", "clada_diag_kernel_times", "clada_device_fault",
                  "clada_threshold_search_cett", "clada_cett_eval", "clada_static_mask_threshold",
                  "clada_static_mask_topk", "clada_static_ffn_decode", "clada_mask_pack", "clada_mask_unpack", "clada_create", "clada_set_option", "clada_prefix_stats", "clada_threshold_calibrate",
                  "clada_cognitive_signals", "clada_threshold", "clada_signals_threshold", "clada_sparse_ffn_decode",
-                 "clada_dense_ffn_decode"):
+                 "clada_dense_ffn_decode", "clada_rope_turns", "clada_qk_rope", "clada_window_attn", "clada_shared_prefix_attn"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -507,6 +539,122 @@ def static_ffn_decode(ctx: Context, layer: Layer, x: torch.Tensor, active_idx: t
     ctx.check(ctx._lib.clada_static_ffn_decode(ctx._h, C.byref(cl), _ptr(x), B, _ptr(active_idx), _ptr(n_active),
                                                _ptr(y), _stream(x)))
     return y
+
+
+def attn_workspace_bytes(B: int, T: int, Hq: int, d: int) -> int:
+    return int(load_library().clada_attn_workspace_bytes(B, T, Hq, d))
+
+
+class KVCache:
+    """Keys and values [batch][heads][capacity][d] on the GPU: two tensors (views with any strides, d contiguous) of one shape and one
+    set of strides.  ring = 0: row n holds position n.  ring > 0: positions from n_sink on share `ring` rows behind the first n_sink."""
+    __slots__ = ("k", "v", "n_sink", "ring", "_c", "_ref")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, n_sink: int = 0, ring: int = 0):
+        shape, stride = k.shape, k.stride()
+        assert k.is_cuda and v.is_cuda and len(shape) == 4 and v.shape == shape and v.dtype == k.dtype and v.device == k.device
+        assert stride[3] == 1 and v.stride() == stride, "k and v need one set of strides, the values of a head contiguous"
+        B, H, N, D = shape
+        self.k, self.v, self.n_sink, self.ring = k, v, n_sink, ring
+        self._c = _CKvCache(k.data_ptr(), v.data_ptr(), stride[0] if B > 1 else 0, stride[1] if H > 1 else 0, stride[2] if N > 1 else 0,
+                            B, H, D, N, _dtype_code(k), n_sink, ring)
+        self._ref = C.byref(self._c)
+
+
+def _heads(x: torch.Tensor, cache: KVCache, what: str):
+    """clada_heads of x [B][T][H][d]."""
+    B, T, H, D = x.shape
+    st = x.stride()
+    assert x.is_cuda and x.dtype == cache.k.dtype and x.device == cache.k.device and D == cache._c.d and st[3] == 1, \
+        f"{what}: type, device, head size or strides do not fit the cache"
+    return C.byref(_CHeads(x.data_ptr(), st[0] if B > 1 else 0, st[1] if T > 1 else 0, st[2] if H > 1 else 0))
+
+
+def _ints(x: torch.Tensor, n: int, cache: KVCache, what: str):
+    assert x.is_cuda and x.dtype == torch.int32 and x.is_contiguous() and x.numel() == n and x.device == cache.k.device, \
+        f"{what}: expected {n} contiguous int32 on the cache's device"
+    return x.data_ptr()
+
+
+@dataclass
+class RopePlan:
+    """Frequencies of a rotation: turns [R/2] int64 on the GPU (the bits of clada_rope.turns), how values pair up, and the factor
+    of cosines and sines.  rope_plan computes one."""
+    turns: torch.Tensor
+    layout: int = ROPE_HALF
+    magnitude: float = 1.0
+
+
+def rope_plan(ctx: Context, rotary_dim: int, theta: float = 10000.0, layout: int = ROPE_HALF, scaling: int = ROPE_SCALE_NONE,
+              factor: float = 1.0, original_len: float = 0.0, low: float = 1.0, high: float = 4.0) -> RopePlan:
+    """Frequencies theta^(-2i/R), scaled for long contexts as clada_rope_turns says (low and high in waves that fit original_len)."""
+    host = torch.empty(max(rotary_dim, 2) // 2, dtype=torch.int64)
+    m = C.c_float()
+    ctx.check(ctx._lib.clada_rope_turns(ctx._h, int(rotary_dim), C.byref(_CRopeScaling(theta, factor, original_len, low, high, scaling)),
+                                        host.data_ptr(), C.byref(m)))
+    return RopePlan(host.to(f"cuda:{ctx.device}"), layout, m.value)
+
+
+def qk_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
+            cache: KVCache, slots: torch.Tensor | None = None, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None,
+            eps: float = 1e-6, norm_offset: float = 0.0, norm: bool | None = None, out: torch.Tensor | None = None):
+    """Norm for each head (norm None: where a weight is given; True without weights: the bare norm), rotation, and keys and values into the cache.  q [B][T][Hq][d], k and v
+    [B][T][heads][d] (any strides, d contiguous), positions [B][T] int32 -> rotated queries (None without q)."""
+    x = q if q is not None else k
+    B, T = x.shape[0], x.shape[1]
+    cq = co = ck = cv = None
+    Hq = 0
+    if q is not None:
+        Hq = q.shape[2]
+        assert q.shape[0] == B and q.shape[1] == T
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        assert out.shape == q.shape
+        cq, co = _heads(q, cache, "q"), _heads(out, cache, "out")
+    if k is not None:
+        assert v is not None and k.shape == v.shape and k.shape[0] == B and k.shape[1] == T and k.shape[2] == cache._c.heads
+        ck, cv = _heads(k, cache, "k"), _heads(v, cache, "v")
+    turns = plan.turns
+    assert turns.is_cuda and turns.dtype == torch.int64 and turns.is_contiguous()
+    c_norm = None
+    if norm or (norm is None and (q_norm is not None or k_norm is not None)):
+        for w in (q_norm, k_norm):
+            assert w is None or (w.is_cuda and w.dtype == x.dtype and w.is_contiguous() and w.numel() == cache._c.d)
+        c_norm = C.byref(_CHeadNorm(_ptr(q_norm), _ptr(k_norm), eps, norm_offset))
+    ctx.check(ctx._lib.clada_qk_rope(ctx._h, C.byref(_CRope(turns.data_ptr(), 2 * turns.numel(), plan.layout, plan.magnitude)), c_norm, B, T, Hq, cq,
+                                     ck, cv, _ints(positions, B * T, cache, "positions"),
+                                     None if slots is None else _ints(slots, B * T, cache, "slots"), co, cache._ref, _stream(x)))
+    return out if q is not None else None
+
+
+def window_attn(ctx: Context, q: torch.Tensor, cache: KVCache, lens: torch.Tensor, q_lens: torch.Tensor | None = None, window: int = 0,
+                sinks: int = 0, scale: float | None = None, out: torch.Tensor | None = None, want_lse: bool = False):
+    """Causal attention of q [B][T][Hq][d] over the cache; lens [B] int32 tokens held (the call's own among them), q_lens [B] int32
+    queries of every sequence (None: T).  window 0: everything is visible.  scale None: d^-0.5.  Returns out, or (out, lse [B][T][Hq])."""
+    B, T, Hq, D = q.shape
+    if out is None:
+        out = torch.empty(B, T, Hq, D, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape
+    lse = torch.empty(B, T, Hq, dtype=torch.float32, device=q.device) if want_lse else None
+    ctx.check(ctx._lib.clada_window_attn(ctx._h, _heads(q, cache, "q"), cache._ref, _ints(lens, B, cache, "lens"),
+                                         None if q_lens is None else _ints(q_lens, B, cache, "q_lens"), B, T, Hq, window, sinks,
+                                         D ** -0.5 if scale is None else scale, _heads(out, cache, "out"), _ptr(lse), _stream(q)))
+    return (out, lse) if want_lse else out
+
+
+def shared_prefix_attn(ctx: Context, q: torch.Tensor, prefix: KVCache, prefix_len: int, cache: KVCache, lens: torch.Tensor,
+                       scale: float | None = None, out: torch.Tensor | None = None, want_lse: bool = False):
+    """One query a sequence, q [B][Hq][d], over the first prefix_len rows of `prefix` (one sequence) and the first lens[b] rows of the
+    sequence's own in `cache`.  Returns out, or (out, lse [B][Hq])."""
+    B, Hq, D = q.shape
+    if out is None:
+        out = torch.empty(B, Hq, D, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and prefix.k.device == cache.k.device
+    lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if want_lse else None
+    ctx.check(ctx._lib.clada_shared_prefix_attn(ctx._h, _heads(q.unsqueeze(1), cache, "q"), prefix._ref, prefix_len, cache._ref,
+                                                _ints(lens, B, cache, "lens"), B, Hq, D ** -0.5 if scale is None else scale,
+                                                _heads(out.unsqueeze(1), cache, "out"), _ptr(lse), _stream(q)))
+    return (out, lse) if want_lse else out
 
 
 def diag_stream_read(ctx: Context, src: torch.Tensor, blocks_per_cu: int = 1):

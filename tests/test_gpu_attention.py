@@ -1,0 +1,230 @@
+"""clada_window_attn and clada_shared_prefix_attn against the plain 64-bit implementation and its rounding bound (attention_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import attention_ref as ref
+from gpu_util import DEV, to_dev, to_np
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def clada():
+    import paper_2502_19078_amd as pkg
+    return pkg
+
+
+@pytest.fixture(scope="module")
+def ctx(clada):
+    return clada.Context(0, clada.attn_workspace_bytes(64, 1024, 64, 256))
+
+
+def _draw(rng, dtype, *shape):
+    return to_dev(rng.standard_normal(shape), dtype)
+
+
+def _ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def _window_case(clada, ctx, dtype, D, Hq, H, T, lens, q_lens, window, sinks, n_sink=0, ring=0, cap=None, seed=0, stale=float("nan"), heads_last=False):
+    """Random queries and cache; rows that no position of the sequence lies in hold `stale`."""
+    rng = np.random.default_rng(seed)
+    B = len(lens)
+    cap = cap or (n_sink + ring if ring else max(max(lens), 1))
+    shape = (B, cap, H, D) if heads_last else (B, H, cap, D)
+    kc, vc = (_draw(rng, dtype, *shape) for _ in range(2))
+    if heads_last:
+        kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
+    for b, n in enumerate(lens):
+        held = torch.zeros(cap, dtype=torch.bool, device=DEV)
+        held[[ref.cache_row(p, n_sink, ring) for p in range(n)]] = True
+        kc[b, :, ~held] = stale
+        vc[b, :, ~held] = stale
+    q = _draw(rng, dtype, B, T, Hq, D)
+    ql = q_lens if q_lens is not None else [T] * B
+    for b in range(B):
+        q[b, ql[b]:] = stale
+    out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc, n_sink, ring), _ints(lens), None if q_lens is None else _ints(q_lens), window, sinks,
+                                 want_lse=True)
+    r = ref.window_attn(to_np(q), to_np(kc), to_np(vc), lens, ql, window, sinks, D ** -0.5, n_sink, ring)
+    ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=T > 1)
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [8, 64, 72, 80, 96, 128, 192, 256])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (6, 2), (8, 1), (20, 1), (40, 1)])
+def test_single_token(clada, ctx, dtype, D, Hq, H):
+    _window_case(clada, ctx, dtype, D, Hq, H, 1, [1, 0, 37, 300, 129], None, 0, 0, seed=D + Hq)
+    _window_case(clada, ctx, dtype, D, Hq, H, 1, [300, 40, 33], None, 32, 4, cap=301, seed=D + Hq + 1, heads_last=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (1, 1), (7, 3), (40, 4), (64, 0), (500, 2), (16, 100)])
+@pytest.mark.parametrize("T", [1, 2, 9, 33, 150])
+def test_windows_and_sinks(clada, ctx, dtype, window, sinks, T):
+    """Lengths shorter than the queries (positions below zero), equal (a prompt), longer (a chunk), zero; ragged queries, none among them."""
+    _window_case(clada, ctx, dtype, 64, 4, 2, T, [T, T + 100, max(T - 1, 0), 0, T + 31], [T, T, T, T, max(T // 2, 0)], window, sinks, seed=T + window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,Hq,H", [(128, 4, 1), (80, 3, 3), (256, 5, 1), (96, 7, 1), (64, 2, 1), (40, 2, 2), (200, 2, 1)])
+@pytest.mark.parametrize("T,extra", [(65, 0), (128, 1), (200, 77), (260, 0)])
+def test_prompts(clada, ctx, dtype, D, Hq, H, T, extra):
+    _window_case(clada, ctx, dtype, D, Hq, H, T, [T + extra, T // 2 + extra], [T, T // 2], 0, 0, seed=T + D)
+    _window_case(clada, ctx, dtype, D, Hq, H, T, [T + extra, T // 3], [T, T // 3], 50, 3, seed=T + D + 1, heads_last=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,window,sinks,n_sink,ring", [(1, 32, 4, 4, 32), (1, 10, 0, 0, 10), (1, 33, 2, 5, 50), (9, 24, 4, 4, 32), (64, 40, 1, 3, 110), (20, 1, 0, 0, 20)])
+def test_rings(clada, ctx, dtype, T, window, sinks, n_sink, ring):
+    """The oldest positions have been written over; lengths before, at and behind each wrap."""
+    for base in (0, n_sink, n_sink + ring - T, n_sink + ring, 3 * ring + 7, 1000003):
+        n = max(base, 0) + T
+        lens = [n, n + 1, n + ring // 2]
+        rng = np.random.default_rng(n)
+        q = _draw(rng, dtype, 3, T, 4, 64)
+        kc, vc = (_draw(rng, dtype, 3, 2, n_sink + ring, 64) for _ in range(2))
+        out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc, n_sink, ring), _ints(lens), None, window, sinks, want_lse=True)
+        # the reference over the positions that matter, moved down to where they are few
+        K, V, Q = to_np(kc), to_np(vc), to_np(q)
+        r = dict(out=np.zeros(Q.shape), lse=np.zeros(Q.shape[:3]), mag=np.zeros(Q.shape), S=np.zeros(Q.shape[:3]), n=np.zeros(Q.shape[:3], int))
+        for b in range(3):
+            for t in range(T):
+                pos = lens[b] - T + t
+                seen = sorted({p for p in range(max(pos - window + 1, 0), pos + 1)} | {p for p in range(min(sinks, pos + 1))})
+                rows = [ref.cache_row(p, n_sink, ring) for p in seen]
+                for h in range(4):
+                    r["out"][b, t, h], r["lse"][b, t, h], r["mag"][b, t, h], r["S"][b, t, h] = ref.attend(Q[b, t, h], K[b, h // 2, rows], V[b, h // 2, rows], 0.125)
+                    r["n"][b, t, h] = len(rows)
+        ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=T > 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("T,window", [(1, 8), (5, 0), (40, 8), (150, 60)])
+def test_what_is_masked_does_not_reach_the_output(clada, ctx, dtype, bad, T, window):
+    """A row of the cache that is not finite reaches the queries that see it and no others."""
+    rng = np.random.default_rng(7)
+    D, Hq, H, n = 64, 4, 2, T + 20
+    q = _draw(rng, dtype, 1, T, Hq, D)
+    kc, vc = (_draw(rng, dtype, 1, H, n, D) for _ in range(2))
+    at = n - 1 - T // 3                                         # seen by the last third at most
+    vc[0, :, at, 5] = bad
+    vc[0, 1, at, 17] = bad
+    out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n]), None, window, 0, want_lse=True)
+    clean = vc.clone()
+    clean[0, :, at] = 0.0
+    r = ref.window_attn(to_np(q), to_np(kc), to_np(clean), [n], [T], window, 0, D ** -0.5)
+    sees = np.array([at <= n - T + t and (window == 0 or at > n - T + t - window) for t in range(T)])
+    want = ref.window_attn(to_np(q), to_np(kc), to_np(vc), [n], [T], window, 0, D ** -0.5)
+    got = to_np(out)
+    assert np.array_equal(np.isnan(got), np.isnan(want["out"])) and np.array_equal(np.isposinf(got), np.isposinf(want["out"]))
+    for t in np.nonzero(~sees)[0]:
+        one = {k: v[:, t:t + 1] for k, v in r.items()}
+        ref.check(got[:, t:t + 1], to_np(lse)[:, t:t + 1], one, dtype, weights_bf16=T > 1)
+    # and a key that is not finite makes the scores of those queries so
+    kc[0, 0, at] = bad
+    out = to_np(clada.window_attn(ctx, q, clada.KVCache(kc, clean), _ints([n]), None, window, 0))
+    assert np.all(np.isfinite(out[0, ~sees]))
+    if bad != bad:
+        assert np.all(np.isnan(out[0, sees][:, :Hq // H]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_scores_and_a_lowest_value(clada, ctx, dtype):
+    """Scores of thousands, and keys of the type's lowest value."""
+    rng = np.random.default_rng(3)
+    D, n = 64, 90
+    q, kc, vc = _draw(rng, dtype, 1, 3, 2, D) * 40, _draw(rng, dtype, 1, 1, n, D) * 40, _draw(rng, dtype, 1, 1, n, D)
+    out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n]), None, 0, 0, want_lse=True)
+    r = ref.window_attn(to_np(q), to_np(kc), to_np(vc), [n], [3], 0, 0, D ** -0.5)
+    ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=True)
+    q = q.abs() * 1e-3
+    kc[0, 0, 10:20] = torch.finfo(kc.dtype).min / 1e3           # scores around -1e36: weights of exactly zero
+    out = clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n]), None, 0, 0)
+    keep = [p for p in range(n) if not 10 <= p < 20]
+    r = ref.window_attn(to_np(q), to_np(kc)[:, :, keep], to_np(vc)[:, :, keep], [n - 10], [3], 0, 0, D ** -0.5)
+    ref.check(to_np(out), None, r, dtype, weights_bf16=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,Hq,H,B", [(128, 8, 2, 3), (64, 4, 4, 1), (80, 5, 5, 17), (256, 8, 1, 5), (96, 6, 3, 40), (64, 40, 2, 2), (128, 16, 1, 64)])
+@pytest.mark.parametrize("P", [1, 31, 500])
+def test_shared_prefix(clada, ctx, dtype, D, Hq, H, B, P):
+    rng = np.random.default_rng(D + B + P)
+    q = _draw(rng, dtype, B, Hq, D)
+    pk, pv = (_draw(rng, dtype, 1, H, P + 3, D) for _ in range(2))
+    kc, vc = (_draw(rng, dtype, B, H, 40, D) for _ in range(2))
+    lens = [int(v) for v in rng.integers(0, 41, B)]
+    lens[0] = 0
+    for c in (pk, pv):
+        c[:, :, P:] = float("nan")
+    for b, n in enumerate(lens):
+        kc[b, :, n:] = float("nan")
+        vc[b, :, n:] = float("nan")
+    out, lse = clada.shared_prefix_attn(ctx, q, clada.KVCache(pk, pv), P, clada.KVCache(kc, vc), _ints(lens), want_lse=True)
+    r = ref.shared_prefix_attn(to_np(q), to_np(pk)[0], to_np(pv)[0], P, to_np(kc), to_np(vc), lens, D ** -0.5)
+    ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=True)
+
+
+def test_strides_and_outputs_in_place_of_others(clada, ctx):
+    """Queries and outputs as slices of wider tensors, the cache with rows of all heads side by side; nothing outside is written."""
+    rng = np.random.default_rng(11)
+    B, T, Hq, H, D, n = 2, 6, 4, 2, 64, 50
+    wide = _draw(rng, "bf16", B, T, Hq + 2 * H, D)
+    q = wide[:, :, :Hq]
+    kc, vc = (_draw(rng, "bf16", B, n, 2 * H, D)[:, :, :H].transpose(1, 2) for _ in range(2))
+    to = torch.full((B, T, Hq + 3, D), 9.0, dtype=torch.bfloat16, device=DEV)
+    clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n, 30]), None, 20, 2, out=to[:, :, 1:Hq + 1])
+    same = clada.window_attn(ctx, q.contiguous(), clada.KVCache(kc.contiguous(), vc.contiguous()), _ints([n, 30]), None, 20, 2)
+    assert torch.equal(to[:, :, 1:Hq + 1], same)
+    assert torch.all(to[:, :, 0] == 9.0) and torch.all(to[:, :, Hq + 1:] == 9.0)
+    # scale, and a broadcast query
+    one = q[:, :1].expand(B, T, Hq, D)
+    a = clada.window_attn(ctx, one, clada.KVCache(kc, vc), _ints([n, 30]), None, 20, 2, scale=0.3)
+    b = clada.window_attn(ctx, one.contiguous(), clada.KVCache(kc, vc), _ints([n, 30]), None, 20, 2, scale=0.3)
+    assert torch.equal(a, b)
+
+
+def test_a_row_past_2_31_values(clada, ctx):
+    """A cache whose rows lie more than 2^31 values, and 2^32 bytes, from its start."""
+    H, D, n = 2, 128, 300
+    step = (2 ** 31 // n // 16 + 1) * 16
+    base = [torch.zeros(step * n + H * D, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    k, v = (torch.as_strided(x, (1, H, n, D), (0, D, step, 1)) for x in base)
+    rng = np.random.default_rng(2)
+    kc, vc = _draw(rng, "bf16", 1, H, n, D), _draw(rng, "bf16", 1, H, n, D)
+    plan = clada.RopePlan(torch.zeros(4, dtype=torch.int64, device=DEV))                # turns of nothing: stored as they are
+    clada.qk_rope(ctx, plan, None, kc.transpose(1, 2), vc.transpose(1, 2), torch.arange(n, dtype=torch.int32, device=DEV)[None], clada.KVCache(k, v))
+    assert torch.equal(k, kc) and torch.equal(v, vc)
+    for T in (1, 70):
+        q = _draw(rng, "bf16", 1, T, 4, D)
+        assert torch.equal(clada.window_attn(ctx, q, clada.KVCache(k, v), _ints([n])), clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n])))
+
+
+@pytest.mark.parametrize("T", [1, 16, 200])
+def test_same_bits_again_on_another_stream_and_in_a_graph(clada, ctx, T):
+    rng = np.random.default_rng(T)
+    B, Hq, H, D, n = 2, 8, 2, 128, 900
+    q, kc, vc = _draw(rng, "bf16", B, T, Hq, D), _draw(rng, "bf16", B, H, n, D), _draw(rng, "bf16", B, H, n, D)
+    cache, lens, out = clada.KVCache(kc, vc), _ints([n, n - 5]), torch.empty_like(q)
+    first = clada.window_attn(ctx, q, cache, lens, window=700, sinks=4)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        again = clada.window_attn(ctx, q, cache, lens, window=700, sinks=4)
+        clada.graph_begin(ctx)
+        clada.window_attn(ctx, q, cache, lens, window=700, sinks=4, out=out)
+        g = clada.graph_end(ctx)
+        for k in range(3):
+            out.zero_()
+            q.neg_()
+            g.launch()
+            s.synchronize()
+            want = clada.window_attn(ctx, q, cache, lens, window=700, sinks=4)
+            assert torch.equal(out, want) and torch.equal(want, first) == (k == 1)
+    s.synchronize()
+    assert torch.equal(first, again)
