@@ -33,7 +33,64 @@ hipError_t clada_attn_rows(const AttnArgs &a, int es, hipStream_t stream);
 hipError_t clada_attn_join(const AttnArgs &a, int es, hipStream_t stream);
 int clada_attn_rows_tile(int rows);                          // rows of a tile of k_attn_rows for so many rows
 
+hipError_t clada_attn_tiles(const AttnArgs &a, hipStream_t stream);     // the prefix's tiles where there are any, else the sequences' own
+
 #ifdef __HIPCC__
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+__device__ __forceinline__ unsigned int pack_bf16(float lo, float hi)      // rounded to nearest even
+{
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    return __builtin_bit_cast(unsigned int, __builtin_convertvector((f32x2{lo, hi}), bf16x2_t));
+}
+
+// Where a row's query and output lie.
+struct RowAt { int64_t q, o, lse; };
+__device__ __forceinline__ RowAt row_at(const AttnArgs &a, bool pre, int b, int h, int r)
+{
+    const int i = r / a.G, hq = h * a.G + (r - i * a.G);
+    const int bb = pre ? i : b, t = pre ? 0 : i;
+    return {bb * a.q_sb + t * a.q_st + hq * a.q_sh, bb * a.o_sb + t * a.o_st + hq * a.o_sh, ((int64_t)bb * a.T + t) * a.Hq + hq};
+}
+
+// Four columns of a transposed read: the 16 lanes of a group name four rows of four values each (lane t: row t / 4, values 4 (t % 4) on) and
+// lane t receives value t of the four rows.
+__device__ __forceinline__ uint2 read_tr16(const char *p)
+{
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)p));
+}
+
+// Values that are not finite.  A weight of zero times such a value is no zero, so a product over a tile would hand it to rows that do not see
+// its key.  A pass whose outputs are not all finite is therefore followed by three more over the same keys: the weights 1 for every
+// key that a row sees, and V with 1 where a value is +inf or NaN (PASS_UP), then -inf or NaN (PASS_DOWN), which count such values for each
+// output; then the plain weights with those values taken out (PASS_REST).  An output with a count is that infinity, or NaN with both.
+enum { PASS_PLAIN = 0, PASS_UP = 1, PASS_DOWN = 2, PASS_REST = 3 };
+template <int ES>
+__device__ __forceinline__ void values_for_pass(u32x4 &v, int pass)
+{
+    if (pass == PASS_PLAIN) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned int w = v[e];
+        if (ES == 4) {
+            const bool odd = (w & 0x7f800000u) == 0x7f800000u, counts = odd && (w << 9 || (w >> 31) == (unsigned int)(pass == PASS_DOWN));
+            v[e] = pass == PASS_REST ? (odd ? 0u : w) : (counts ? 0x3f800000u : 0u);
+        } else {
+            unsigned int r = 0;
+#pragma unroll
+            for (int s = 0; s < 32; s += 16) {
+                const unsigned int x = w >> s & 0xffffu;
+                const bool odd = (x & 0x7f80u) == 0x7f80u, counts = odd && ((x & 0x7fu) || (x >> 15) == (unsigned int)(pass == PASS_DOWN));
+                r |= (pass == PASS_REST ? (odd ? 0u : x) : (counts ? 0x3f80u : 0u)) << s;
+            }
+            v[e] = r;
+        }
+    }
+}
+
 // The keys that a tile's rows may see, in order: `head` sinks from position 0 on, then the positions from `lo` on.
 struct KeyRange {
     int n, head, lo;         // keys in all

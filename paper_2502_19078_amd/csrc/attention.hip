@@ -18,30 +18,7 @@
 
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-
 constexpr float NEG_INF = -INFINITY;
-
-__device__ __forceinline__ unsigned int pack_bf16(float lo, float hi)
-{
-    return f32_to_bf16_bits(lo) | (f32_to_bf16_bits(hi) << 16);
-}
-
-__device__ __forceinline__ bool finite_bf16x2(unsigned int v)
-{
-    return (v & 0x7f80u) != 0x7f80u && (v & 0x7f800000u) != 0x7f800000u;
-}
-
-// Where a row's query and output lie.
-struct RowAt { int64_t q, o, lse; };
-__device__ __forceinline__ RowAt row_at(const AttnArgs &a, bool pre, int b, int h, int r)
-{
-    const int i = r / a.G, hq = h * a.G + (r - i * a.G);
-    const int bb = pre ? i : b, t = pre ? 0 : i;
-    return {bb * a.q_sb + t * a.q_st + hq * a.q_sh, bb * a.o_sb + t * a.o_st + hq * a.o_sh, ((int64_t)bb * a.T + t) * a.Hq + hq};
-}
 
 // ES: bytes a value.  DP: D rounded up to the products' tiles; FULL: D == DP.  NT: tiles of 16 rows.
 template <int ES, int DP, int NT, bool FULL>
@@ -160,10 +137,8 @@ k_attn_rows(const AttnArgs a)
         }
     };
 
-    // A weight of zero, or the lower half of one, times a value that is not finite is no zero: the products alone would hand such values to rows
-    // that do not see them, and turn infinities into NaNs.  Outputs that are not finite are therefore computed a second time with those values
-    // taken out of the products and added for the rows that see them.
-    for (int careful = 0; careful < 2; ++careful) {
+    unsigned int up[NT][(4 * DB + 31) / 32], down[NT][(4 * DB + 31) / 32];     // a bit for every output
+    for (int pass = PASS_PLAIN; pass <= PASS_REST; ++pass) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt] = NEG_INF;
@@ -196,21 +171,9 @@ k_attn_rows(const AttnArgs a)
             }
         const int p_first = kr.pos(i), p_last = kr.pos(min(i + KS, k1) - 1);
         const bool mixed = !one_pos && !(p_last <= kr.pos_a && (a.window == 0 || p_first > kr.pos_b - a.window || p_last < a.sinks));
-        bool odd_v = false;
-        if (careful) {
-            bool ok = true;
+        if (pass) {
 #pragma unroll
-            for (int j = 0; j < VL; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    unsigned int w = vf[j][e];
-                    if (ES == 2) {
-                        if ((w & 0x7f80u) == 0x7f80u) { ok = false; w &= 0xffff0000u; }
-                        if ((w & 0x7f800000u) == 0x7f800000u) { ok = false; w &= 0xffffu; }
-                    } else if ((w & 0x7f800000u) == 0x7f800000u) { ok = false; w = 0; }
-                    vf[j][e] = w;
-                }
-            odd_v = __any(!ok);
+            for (int j = 0; j < VL; ++j) values_for_pass<ES>(vf[j], pass);
         }
         if (ES == 2) {
 #pragma unroll
@@ -235,7 +198,7 @@ k_attn_rows(const AttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int key = i + kb * 16 + 4 * g + e;
-                    float x = s[nt][kb][e] * a.scale2;
+                    float x = pass == PASS_UP || pass == PASS_DOWN ? 0.0f : s[nt][kb][e] * a.scale2;
                     bool see = key < k1;
                     if (mixed) {
                         const int p = kr.pos(key);
@@ -280,9 +243,7 @@ k_attn_rows(const AttnArgs a)
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const char *src = my_v + (4 * g + (n16 >> 2)) * PITCH + d * 32 + (n16 & 3) * 8;
-                const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)src);
-                const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(src + 16 * PITCH));
-                const uint2 u0 = __builtin_bit_cast(uint2, v0), u1 = __builtin_bit_cast(uint2, v1);
+                const uint2 u0 = read_tr16(src), u1 = read_tr16(src + 16 * PITCH);
                 const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y});
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -301,43 +262,34 @@ k_attn_rows(const AttnArgs a)
                         o[nt][(j / 4 * 4 + e) % DB] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vv), s[nt][0][j % 4], o[nt][(j / 4 * 4 + e) % DB], 0, 0, 0);
                     }
         }
-        if (odd_v) {
-            for (int key = 0; key < KS && i + key < k1; ++key) {
-                const int p = kr.pos(i + key);
-                const char *row = vp + kr.row(p, kv) * kv.sn;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float w = 0.0f;
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (key >> 4 == kb && (key & 3) == e) w = s[nt][kb][e];
-                    w = __shfl(w, ((key & 15) >> 2) * 16 + n16);
-                    const bool see = one_pos || (p <= row_pos[nt] && (a.window == 0 || p > row_pos[nt] - a.window || p < a.sinks));
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int dim = ES == 2 ? 16 * d + 4 * g + e : 64 * (d / 4) + 4 * (4 * g + e) + d % 4;
-                            if (!FULL && dim >= Dd) continue;
-                            const float v = ES == 2 ? __uint_as_float((unsigned int)reinterpret_cast<const unsigned short *>(row)[dim] << 16)
-                                                    : reinterpret_cast<const float *>(row)[dim];
-                            if (see && !(fabsf(v) < INFINITY)) o[nt][d][e] += w * v;
-                        }
-                }
-            }
-        }
     }
-
-    bool fine = true;
+    if (pass == PASS_PLAIN) {
+        bool fine = true;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) fine = fine && fabsf(o[nt][d][e]) < INFINITY;
+        if (__all(fine)) break;
+        continue;
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) fine = fine && fabsf(o[nt][d][e]) < INFINITY;
-    if (__all(fine)) break;
+            for (int e = 0; e < 4; ++e) {
+                const int w = (4 * d + e) / 32, bit = (4 * d + e) % 32;
+                if (bit == 0 && pass == PASS_UP) up[nt][w] = 0;
+                if (bit == 0 && pass == PASS_DOWN) down[nt][w] = 0;
+                if (pass == PASS_UP) up[nt][w] |= (o[nt][d][e] > 0.0f ? 1u : 0u) << bit;
+                else if (pass == PASS_DOWN) down[nt][w] |= (o[nt][d][e] > 0.0f ? 1u : 0u) << bit;
+                else {
+                    if (up[nt][w] >> bit & 1) o[nt][d][e] += INFINITY;
+                    if (down[nt][w] >> bit & 1) o[nt][d][e] -= INFINITY;
+                }
+            }
     }
 
     // join the waves: 2 and 3 hand over to 0 and 1, then 1 to 0

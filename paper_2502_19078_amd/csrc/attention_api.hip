@@ -136,7 +136,9 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     a.q_lens = q_lens;
     a.window = window;
     a.sinks = window ? sinks : 0;
-    const int es = (int)dtype_size(cache->dtype), tile = clada_attn_rows_tile(T * a.G);
+    const int es = (int)dtype_size(cache->dtype);
+    const bool many = es == 2 && T * a.G >= 64;
+    const int tile = many ? 128 : clada_attn_rows_tile(T * a.G);
     a.own_tiles = (T * a.G + tile - 1) / tile;
     const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
     int64_t keys = cache->capacity;                          // what a tile can see at most
@@ -147,7 +149,7 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     a.splits = splits_for(units, keys, ctx->num_cu);
     if (units * a.splits > INT32_MAX) return clada_fail(ctx, CLADA_ERR_SHAPE, "the call has too many rows");
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
-    CLADA_CHECK_HIP(ctx, clada_attn_rows(a, es, (hipStream_t)hip_stream));
+    CLADA_CHECK_HIP(ctx, many ? clada_attn_tiles(a, (hipStream_t)hip_stream) : clada_attn_rows(a, es, (hipStream_t)hip_stream));
     if (a.splits > 1) CLADA_CHECK_HIP(ctx, clada_attn_join(a, es, (hipStream_t)hip_stream));
     return CLADA_OK;
 }

@@ -1,0 +1,291 @@
+// bf16 attention for many rows: prompts, long chunks, and a shared prefix read for a large batch.
+//
+// The same sums as in attention.hip, bound by the matrix cores and the vector units: a tile of 32 rows by 64 keys is 32 products of
+// 32x32x16 (1024 clocks of a SIMD at 128 values a head) beside 32 exponentials, maxima, sums and conversions a lane (about as many clocks
+// again).  A workgroup of four waves takes 128 rows, 32 a wave; K and V tiles of 64 keys go through registers into one of two LDS buffers while
+// the other is multiplied, one barrier a tile.  Two workgroups share a compute unit, so one's products run under the other's exponentials.
+//
+// Scores are formed transposed (S^T = K Q^T): a lane holds scores of one row only, keys 8 (i / 4) + 4 (lane / 32) + i % 4 of each 32, and the same
+// registers, rounded to bf16, are the second operand of O^T = V^T P^T when its keys are counted in that order (V is turned by
+// ds_read_tr16).  The weights' rounding (2^-8 at most, to nearest) is of the size of the output's own; their sum is taken before it.
+#include <math.h>
+
+#include "attention.h"
+
+namespace {
+
+constexpr float NEG_INF = -INFINITY;
+
+// Orders the LDS accesses around it; leaves loads from memory in flight.
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int DP, bool FULL>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
+k_attn_tiles(const AttnArgs a)
+{
+    constexpr int KT = DP <= 128 ? 64 : 32, KB = KT / 32;    // keys of a tile
+    constexpr int KD = DP / 16, DB = DP / 32;
+    constexpr int CPR = DP / 8, ROWS = KT * CPR / 256;       // 16-byte chunks of a row; chunks of K (and of V) a thread stages
+    constexpr int KP = DP * 2 + 16, VP = DP * 2 + 32;        // row pitches: K rows 4 banks apart, V rows 8
+    constexpr int BUF = KT * (KP + VP);
+    static_assert(KT * CPR % 256 == 0, "whole passes");
+    __shared__ __align__(16) char lds[2 * BUF];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n32 = lane & 31, hh = lane >> 5, t16 = lane & 15, g = lane >> 4;
+    const int Dd = FULL ? DP : a.D;
+
+    // Units (sequence, key head) fastest: consecutive workgroups go to different XCDs, so a unit's tiles share an L2.  The last row tiles see the
+    // most keys and come first.
+    const bool pre = a.pre_tiles != 0;
+    const int units = pre ? a.Hkv : a.B * a.Hkv, tiles = pre ? a.pre_tiles : a.own_tiles, splits = pre ? a.pre_splits : a.splits;
+    const int unit = blockIdx.x % units, rest = blockIdx.x / units;
+    const int split = rest % splits, tile = tiles - 1 - rest / splits;
+    const int h = unit % a.Hkv, b = unit / a.Hkv;
+    const int rows = (pre ? a.B : a.T) * a.G, r0 = tile * 128;
+    const AttnKV &kv = pre ? a.pre : a.kv;
+    KeyRange kr;
+    int first_pos = 0, qlen = a.T;
+    if (pre) {
+        kr.n = a.pre_n;
+        kr.head = kr.lo = kr.ring_base = 0;
+        kr.pos_a = kr.pos_b = a.pre_n;
+    } else {
+        int len;
+        sequence_lens(a, b, len, qlen);
+        first_pos = len - qlen;
+        kr = key_range(kv, first_pos, r0 / a.G, min(min(r0 + 127, rows - 1) / a.G, qlen - 1), a.window, a.sinks);
+    }
+    int chunk = (kr.n + splits - 1) / splits;
+    chunk = (chunk + KT - 1) / KT * KT;
+    const int k0 = min(split * chunk, kr.n), k1 = min(k0 + chunk, kr.n);
+
+    // this lane's row
+    const int r = r0 + wave * 32 + n32, rc = min(r, rows - 1);
+    const RowAt at = row_at(a, pre, b, h, rc);
+    const int row_pos = pre ? a.pre_n : rc / a.G < qlen ? first_pos + rc / a.G : -1;
+    // positions of the wave's first and last row, for tiles that all or none of its rows see
+    const int wr0 = min(r0 + wave * 32, rows - 1), wr1 = min(r0 + wave * 32 + 31, rows - 1);
+    const int wave_a = pre ? a.pre_n : wr0 / a.G < qlen ? first_pos + wr0 / a.G : -1;
+    const int wave_b = pre ? a.pre_n : min(wr1 / a.G, qlen - 1) + first_pos;
+    const bool ragged = !pre && wr1 / a.G >= qlen;           // rows of padding among them
+
+    const unsigned int flip = a.scale2 < 0.0f ? 0x80008000u : 0u;      // a negative scale is the queries' sign
+    const float scale2 = fmaxf(fabsf(a.scale2), 1e-37f);     // (positive, so that -inf stays what it is)
+    u32x4 qf[KD];
+#pragma unroll
+    for (int c = 0; c < KD; ++c) {
+        const int off = 32 * c + 16 * hh;
+        const bool in = FULL || off < Dd * 2;
+        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + at.q + (in ? off : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qf[c][e] = in ? qf[c][e] ^ flip : 0u;
+    }
+
+    const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
+    u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
+    auto fetch = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            const int id = tid + 256 * j, key = i + id / CPR, col = id % CPR * 16;
+            const bool in = FULL || col < Dd * 2;
+            const int64_t off = kr.row(kr.pos(min(key, k1 - 1)), kv) * kv.sn + (in ? col : 0);
+            sk[j] = *reinterpret_cast<const u32x4 *>(kp + off);
+            sv[j] = *reinterpret_cast<const u32x4 *>(vp + off);
+            if (!in) sk[j] = u32x4{0, 0, 0, 0};
+            if (!in || key >= k1) sv[j] = u32x4{0, 0, 0, 0};
+        }
+    };
+    auto put = [&](int buf) {
+        char *to = lds + buf * BUF;
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            const int id = tid + 256 * j, key = id / CPR, col = id % CPR * 16;
+            *reinterpret_cast<u32x4 *>(to + key * KP + col) = sk[j];
+            *reinterpret_cast<u32x4 *>(to + KT * KP + key * VP + col) = sv[j];
+        }
+    };
+
+    f32x16 o[DB];
+    float m, l;
+    unsigned int up[DB], down[DB];                           // halfwords of a bit for every output
+    for (int pass = PASS_PLAIN; pass <= PASS_REST; ++pass) {
+        m = NEG_INF;
+        l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+        auto shape = [&]() {
+            if (pass) {
+#pragma unroll
+                for (int j = 0; j < ROWS; ++j) values_for_pass<2>(sv[j], pass);
+            }
+        };
+        if (k0 < k1) {
+            fetch(k0);
+            shape();
+            put(0);
+            if (k0 + KT < k1) fetch(k0 + KT);
+        }
+        tile_barrier();
+        int buf = 0;
+        for (int i = k0; i < k1; i += KT, buf ^= 1) {
+            const int last = min(i + KT, k1) - 1, p_first = kr.pos(i), p_last = kr.pos(last);
+            // (a tile that begins among the sinks is looked at key by key)
+            const bool none = p_first > wave_b || (a.window && p_first >= a.sinks && p_last <= wave_a - a.window && wave_a >= 0);
+            const bool all = last == i + KT - 1 && !ragged && (pre || (p_last <= wave_a && (a.window == 0 || p_first > wave_b - a.window || p_last < a.sinks)));
+            if (!none) {
+                const char *kb = lds + buf * BUF, *vb = kb + KT * KP;
+                f32x16 s[KB];
+#pragma unroll
+                for (int k = 0; k < KB; ++k) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[k][e] = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < KD; ++c) {
+                        const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
+                        s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), s[k], 0, 0, 0);
+                    }
+                }
+                if (pass == PASS_UP || pass == PASS_DOWN) {
+#pragma unroll
+                    for (int k = 0; k < KB; ++k)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[k][e] = 0.0f;
+                }
+                if (!all) {
+#pragma unroll
+                    for (int k = 0; k < KB; ++k)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int key = i + k * 32 + 8 * (e >> 2) + 4 * hh + (e & 3), p = kr.pos(key);
+                            const bool see = key < k1 && p <= row_pos && (pre || a.window == 0 || p > row_pos - a.window || p < a.sinks);
+                            s[k][e] = see ? s[k][e] : NEG_INF;
+                        }
+                }
+                float top = NEG_INF;
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
+                top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
+                // The maximum moves only when it is passed by a factor of 2^8: weights stay below 2^8, where fp32 and bf16 lose nothing.
+                if (__any(top > m + 8.0f)) {
+                    const float mn = fmaxf(m, top);
+                    const float f = mn == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+                    m = mn;
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d] *= f;
+                }
+                const float base = m == NEG_INF ? 0.0f : m;
+                unsigned int pk[KB][8];
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[k][e], scale2, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[k][e + 1], scale2, -base));
+                        l += p0 + p1;
+                        pk[k][e >> 1] = pack_bf16(p0, p1);
+                    }
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pk[k][4 * c], pk[k][4 * c + 1], pk[k][4 * c + 2], pk[k][4 * c + 3]});
+                        const char *src = vb + (k * 32 + c * 16 + 4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
+#pragma unroll
+                        for (int d = 0; d < DB; ++d) {
+                            const uint2 u0 = read_tr16(src + d * 64), u1 = read_tr16(src + d * 64 + 8 * VP);
+                            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y}), pf, o[d], 0, 0, 0);
+                        }
+                    }
+            }
+            if (i + KT < k1) {
+                shape();
+                put(buf ^ 1);
+                if (i + 2 * KT < k1) fetch(i + 2 * KT);
+            }
+            tile_barrier();
+        }
+        if (pass == PASS_PLAIN) {
+            bool fine = true;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) fine = fine && fabsf(o[d][e]) < INFINITY;
+            if (!__syncthreads_or(!fine)) break;
+            continue;
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            if (pass == PASS_UP) up[d] = 0;
+            if (pass == PASS_DOWN) down[d] = 0;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (pass == PASS_UP) up[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
+                else if (pass == PASS_DOWN) down[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
+                else {
+                    if (up[d] >> e & 1) o[d][e] += INFINITY;
+                    if (down[d] >> e & 1) o[d][e] -= INFINITY;
+                }
+            }
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (r >= rows) return;
+
+    const int all_splits = a.splits + a.pre_splits;
+    if (all_splits > 1) {
+        const int64_t part = at.lse * all_splits + split;
+        if (hh == 0) a.part_ml[part] = make_float2(m, l);
+        if (k0 == k1) return;
+        float *to = a.part_o + part * Dd;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int dim = 32 * d + 2 * e + 4 * hh;
+                if (FULL || dim < Dd) *reinterpret_cast<f32x4 *>(to + dim) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+            }
+        return;
+    }
+    const bool nothing = kr.n == 0 || row_pos < 0;
+    if (a.lse && hh == 0) a.lse[at.lse] = nothing ? NEG_INF : (m == NEG_INF ? NEG_INF : m * 0.69314718055994531f) + logf(l);
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int dim = 32 * d + 2 * e + 4 * hh;
+            if (!FULL && dim >= Dd) continue;
+            const uint2 v = make_uint2(pack_bf16(o[d][e] * inv, o[d][e + 1] * inv), pack_bf16(o[d][e + 2] * inv, o[d][e + 3] * inv));
+            *reinterpret_cast<uint2 *>(a.out + at.o + dim * 2) = nothing ? make_uint2(0, 0) : v;
+        }
+}
+
+template <int DP>
+void launch_tiles(const AttnArgs &a, hipStream_t stream)
+{
+    const int64_t blocks = a.pre_tiles ? (int64_t)a.Hkv * a.pre_tiles * a.pre_splits : (int64_t)a.B * a.Hkv * a.own_tiles * a.splits;
+    const dim3 grid((unsigned int)blocks), block(256);
+    if (a.D == DP) hipLaunchKernelGGL((k_attn_tiles<DP, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((k_attn_tiles<DP, false>), grid, block, 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t clada_attn_tiles(const AttnArgs &a, hipStream_t stream)
+{
+    if (a.D <= 64) launch_tiles<64>(a, stream);
+    else if (a.D <= 96) launch_tiles<96>(a, stream);
+    else if (a.D <= 128) launch_tiles<128>(a, stream);
+    else launch_tiles<256>(a, stream);
+    return hipGetLastError();
+}
