@@ -29,17 +29,18 @@ struct AttnArgs {
     float *part_o;
 };
 
-hipError_t clada_attn_rows(const AttnArgs &a, int es, hipStream_t stream);
-hipError_t clada_attn_join(const AttnArgs &a, int es, hipStream_t stream);
-int clada_attn_rows_tile(int rows);                          // rows of a tile of k_attn_rows for so many rows
-
-hipError_t clada_attn_tiles(const AttnArgs &a, hipStream_t stream);     // the prefix's tiles where there are any, else the sequences' own
+// Which kernel: tiles of 16 rows (both types), 32 rows (fp32), 128 rows (bf16); a shared prefix in tiles of 128 rows with the
+// sequences' own keys in tiles of 16 (bf16).  Partial results are joined where there are any.
+enum AttnPath { ATTN_ROWS16, ATTN_ROWS32, ATTN_TILES, ATTN_PREFIX };
+hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, hipStream_t stream);
 
 #ifdef __HIPCC__
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+constexpr float NEG_INF = -__builtin_inff();
 
 __device__ __forceinline__ unsigned int pack_bf16(float lo, float hi)      // rounded to nearest even
 {

@@ -1,366 +1,39 @@
-// Attention over a key / value cache for few rows (clada_window_attn's single tokens and short chunks, clada_shared_prefix_attn, and all
-// fp32 calls), and the entry points.
-//
-// For a row r and the keys p that it may see:  o_r = sum_p exp(s_rp - lse_r) v_p,  s_rp = scale q_r . k_p,  lse_r = log sum_p exp(s_rp).
-// One pass over the keys with a running maximum and sum per row, in base 2.
-//
-// Bound by the cache's bytes (HBM): a key head's rows of the cache are read once for all query heads of its group.  A workgroup takes a tile
-// of 16 or 32 rows and one split of their keys; its four waves take 32 (fp32: 16) keys in turn, each with a running softmax of its own, so
-// nothing waits inside the loop; the waves' results are joined through LDS, those of the splits by k_attn_join.
-//
-// Scores are formed transposed, S^T = K Q^T: a lane then holds scores of one row only, keys 4 (lane / 16) + i of each 16, and the same
-// registers are the operand of O^T = V^T P^T when its keys are counted in that order.  K goes from memory into the operand registers as it
-// lies; bf16 V goes through LDS, where ds_read_tr16 turns it; fp32 V needs no turning.  The weights enter the second product as two bf16, 16
-// bits: the matrix cores have time to spare here.
+// Kernels of clada_window_attn and clada_shared_prefix_attn: few rows (single tokens) run attention_rows.h, many attention_tiles.h; where
+// a row's keys are split among workgroups, k_attn_join adds their results up in a second launch.
 #include <math.h>
 
-#include "attention.h"
+#include "attention_rows.h"
+#include "attention_tiles.h"
 
 namespace {
 
-constexpr float NEG_INF = -INFINITY;
-
-// ES: bytes a value.  DP: D rounded up to the products' tiles; FULL: D == DP.  NT: tiles of 16 rows.
 template <int ES, int DP, int NT, bool FULL>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, ES == 2 && DP <= 128 ? 2 : 1)
 k_attn_rows(const AttnArgs a)
 {
-    constexpr int CH = DP * ES / 64;                         // chunks of 64 bytes in a row: lane group g holds 16 bytes of each
-    constexpr int KB = ES == 2 ? 2 : 1, KS = 16 * KB;        // keys of a step
-    constexpr int DB = DP / 16;                              // tiles of 16 output dimensions
-    constexpr int CPR = DP * ES / 16;                        // 16-byte chunks of a row
-    constexpr int VL = KS * CPR / 64;                        // 16-byte loads of V a lane and step
-    constexpr int PITCH = DP * 2 + 32;                       // V in LDS: rows 8 banks apart modulo 64
-    constexpr int V_LDS = ES == 2 ? 4 * 32 * PITCH : 0, J_LDS = 2 * NT * 16 * (DP * 4 + 8);
-    __shared__ __align__(16) char lds[V_LDS > J_LDS ? V_LDS : J_LDS];
+    __shared__ __align__(16) char lds[RowsShape<ES, DP, NT>::LDS];
+    const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
+    attn_rows<ES, DP, NT, FULL>(a, id < pre_blocks, id < pre_blocks ? id : id - pre_blocks, lds);
+}
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n16 = lane & 15, g = lane >> 4;
-    const int Dd = FULL ? DP : a.D;
+template <int DP, bool FULL>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
+k_attn_tiles(const AttnArgs a)
+{
+    __shared__ __align__(16) char lds[TilesShape<DP>::LDS];
+    attn_tiles<DP, FULL>(a, false, blockIdx.x, lds);
+}
 
-    // which tile of which keys
-    int id = blockIdx.x, split, b = 0, h, tile, splits, rows;
-    const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits;
-    const bool pre = id < pre_blocks;
-    if (pre) {
-        split = id % a.pre_splits;
-        id /= a.pre_splits;
-        tile = id % a.pre_tiles;
-        h = id / a.pre_tiles;
-        splits = a.pre_splits;
-        rows = a.B * a.G;
-    } else {
-        id -= pre_blocks;
-        split = id % a.splits;
-        id /= a.splits;
-        tile = id % a.own_tiles;
-        id /= a.own_tiles;
-        h = id % a.Hkv;
-        b = id / a.Hkv;
-        splits = a.splits;
-        rows = a.T * a.G;
-    }
-    const int all_splits = a.splits + a.pre_splits, part = pre ? split : a.pre_splits + split;
-    const int r0 = tile * 16 * NT;
-    const AttnKV &kv = pre ? a.pre : a.kv;
-    KeyRange kr;
-    int first_pos = 0, qlen = a.T;
-    if (pre) {
-        kr.n = a.pre_n;
-        kr.head = kr.lo = kr.ring_base = 0;
-        kr.pos_a = kr.pos_b = a.pre_n;
-    } else {
-        int len;
-        sequence_lens(a, b, len, qlen);
-        first_pos = len - qlen;
-        if (a.pre_splits) {                                  // behind a prefix: all of the sequence's rows
-            kr = key_range(kv, len - 1, 0, 0, 0, 0);
-        } else
-            kr = key_range(kv, first_pos, r0 / a.G, min(min(r0 + 16 * NT - 1, rows - 1) / a.G, qlen - 1), a.window, a.sinks);
-    }
-    const bool one_pos = pre || a.pre_splits || kr.pos_a == kr.pos_b;      // all rows see the same keys
-    int chunk = (kr.n + splits - 1) / splits;
-    chunk = (chunk + 31) & ~31;
-    const int k0 = min(split * chunk, kr.n), k1 = min(k0 + chunk, kr.n);
-
-    // this lane's rows: queries as the second operand, and the positions that they may see
-    u32x4 qf[NT][CH];
-    int row_pos[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = r0 + nt * 16 + n16;
-        const RowAt at = row_at(a, pre, b, h, min(r, rows - 1));
-        const int i = min(r, rows - 1) / a.G;
-        row_pos[nt] = pre || a.pre_splits ? 0 : i < qlen ? first_pos + i : -1;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int off = 64 * c + 16 * g;
-            const bool in = FULL || off < Dd * ES;
-            qf[nt][c] = *reinterpret_cast<const u32x4 *>(a.q + at.q + (in ? off : 0));
-            if (!in) qf[nt][c] = u32x4{0, 0, 0, 0};
-        }
-    }
-
-    const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
-    char *my_v = lds + wave * 32 * PITCH;
-
-    f32x4 o[NT][DB];
-    float m[NT], l[NT];
-    u32x4 kf[KB][CH], vf[VL];
-    auto load = [&](int i) {                                 // keys i .. i + KS - 1; past the end the last one again
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            const char *p = kp + kr.row(kr.pos(min(i + kb * 16 + n16, k1 - 1)), kv) * kv.sn;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int off = 64 * c + 16 * g;
-                const bool in = FULL || off < Dd * ES;
-                kf[kb][c] = *reinterpret_cast<const u32x4 *>(p + (in ? off : 0));
-                if (!in) kf[kb][c] = u32x4{0, 0, 0, 0};
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < VL; ++j) {
-            int key, col;                                    // bf16: chunks in order of the rows, for LDS; fp32: key 4 g + i, 64 values a load
-            if (ES == 2) {
-                const int id = lane + 64 * j;
-                key = id / CPR;
-                col = id % CPR;
-            } else {
-                key = 4 * g + j % 4;
-                col = 16 * (j / 4) + n16;
-            }
-            const bool in = FULL || col * 16 < Dd * ES;
-            const char *p = vp + kr.row(kr.pos(min(i + key, k1 - 1)), kv) * kv.sn;
-            vf[j] = *reinterpret_cast<const u32x4 *>(p + (in ? col * 16 : 0));
-            if (!in || i + key >= k1) vf[j] = u32x4{0, 0, 0, 0};
-        }
-    };
-
-    unsigned int up[NT][(4 * DB + 31) / 32], down[NT][(4 * DB + 31) / 32];     // a bit for every output
-    for (int pass = PASS_PLAIN; pass <= PASS_REST; ++pass) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = NEG_INF;
-        l[nt] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[nt][d] = f32x4{0, 0, 0, 0};
-    }
-    int i = k0 + wave * KS;
-    if (i < k1) load(i);
-    for (; i < k1; i += 4 * KS) {
-        // scores of KS keys: lane holds keys 16 kb + 4 g + e of its row
-        f32x4 s[NT][KB];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                s[nt][kb] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    if (ES == 2)
-                        s[nt][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[kb][c]),
-                                                                            __builtin_bit_cast(bf16x8, qf[nt][c]), s[nt][kb], 0, 0, 0);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const unsigned int ka = kf[kb][c][e], qb = qf[nt][c][e];
-                            s[nt][kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(ka), __uint_as_float(qb), s[nt][kb], 0, 0, 0);
-                        }
-                }
-            }
-        const int p_first = kr.pos(i), p_last = kr.pos(min(i + KS, k1) - 1);
-        const bool mixed = !one_pos && !(p_last <= kr.pos_a && (a.window == 0 || p_first > kr.pos_b - a.window || p_last < a.sinks));
-        if (pass) {
-#pragma unroll
-            for (int j = 0; j < VL; ++j) values_for_pass<ES>(vf[j], pass);
-        }
-        if (ES == 2) {
-#pragma unroll
-            for (int j = 0; j < VL; ++j) {
-                const int id = lane + 64 * j;
-                *reinterpret_cast<u32x4 *>(my_v + id / CPR * PITCH + id % CPR * 16) = vf[j];
-            }
-        }
-        u32x4 va[ES == 4 ? VL : 1];
-        if (ES == 4)
-#pragma unroll
-            for (int j = 0; j < VL; ++j) va[ES == 4 ? j : 0] = vf[j];
-        const int next = i + 4 * KS;
-        if (next < k1) load(next);
-        __builtin_amdgcn_wave_barrier();
-
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float top = NEG_INF;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = i + kb * 16 + 4 * g + e;
-                    float x = pass == PASS_UP || pass == PASS_DOWN ? 0.0f : s[nt][kb][e] * a.scale2;
-                    bool see = key < k1;
-                    if (mixed) {
-                        const int p = kr.pos(key);
-                        see = see && p <= row_pos[nt] && (a.window == 0 || p > row_pos[nt] - a.window || p < a.sinks);
-                    }
-                    x = see ? x : NEG_INF;
-                    s[nt][kb][e] = x;
-                    top = fmaxf(top, x);
-                }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (__any(top > m[nt])) {
-                const float mn = fmaxf(m[nt], top);
-                const float f = mn == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - mn);
-                m[nt] = mn;
-                l[nt] *= f;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[nt][d] *= f;
-            }
-            const float base = m[nt] == NEG_INF ? 0.0f : m[nt];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(s[nt][kb][e] - base);
-                    s[nt][kb][e] = p;
-                    l[nt] += p;
-                }
-        }
-
-        if (ES == 2) {
-            u32x4 hi[NT], lo[NT];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float p0 = s[nt][(w >> 1) % KB][2 * (w & 1)], p1 = s[nt][(w >> 1) % KB][2 * (w & 1) + 1];
-                    const unsigned int u = pack_bf16(p0, p1);
-                    hi[nt][w] = u;
-                    lo[nt][w] = pack_bf16(p0 - __uint_as_float(u << 16), p1 - __uint_as_float(u & 0xffff0000u));
-                }
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const char *src = my_v + (4 * g + (n16 >> 2)) * PITCH + d * 32 + (n16 & 3) * 8;
-                const uint2 u0 = read_tr16(src), u1 = read_tr16(src + 16 * PITCH);
-                const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y});
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    o[nt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, hi[nt]), o[nt][d], 0, 0, 0);
-                    o[nt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, lo[nt]), o[nt][d], 0, 0, 0);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < VL; ++j)                     // keys 4 g + j % 4, dimensions 64 (j / 4) + 4 n16 + e
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const unsigned int vv = va[ES == 4 ? j : 0][e];
-                        o[nt][(j / 4 * 4 + e) % DB] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vv), s[nt][0][j % 4], o[nt][(j / 4 * 4 + e) % DB], 0, 0, 0);
-                    }
-        }
-    }
-    if (pass == PASS_PLAIN) {
-        bool fine = true;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) fine = fine && fabsf(o[nt][d][e]) < INFINITY;
-        if (__all(fine)) break;
-        continue;
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int w = (4 * d + e) / 32, bit = (4 * d + e) % 32;
-                if (bit == 0 && pass == PASS_UP) up[nt][w] = 0;
-                if (bit == 0 && pass == PASS_DOWN) down[nt][w] = 0;
-                if (pass == PASS_UP) up[nt][w] |= (o[nt][d][e] > 0.0f ? 1u : 0u) << bit;
-                else if (pass == PASS_DOWN) down[nt][w] |= (o[nt][d][e] > 0.0f ? 1u : 0u) << bit;
-                else {
-                    if (up[nt][w] >> bit & 1) o[nt][d][e] += INFINITY;
-                    if (down[nt][w] >> bit & 1) o[nt][d][e] -= INFINITY;
-                }
-            }
-    }
-
-    // join the waves: 2 and 3 hand over to 0 and 1, then 1 to 0
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        l[nt] += __shfl_xor(l[nt], 16);
-        l[nt] += __shfl_xor(l[nt], 32);
-    }
-#pragma unroll
-    for (int step = 2; step >= 1; step >>= 1) {
-        __syncthreads();
-        if (wave >= step && wave < 2 * step) {
-            char *to = lds + (wave - step) * NT * 16 * (DP * 4 + 8);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d) reinterpret_cast<f32x4 *>(to)[(nt * DB + d) * 64 + lane] = o[nt][d];
-                if (g == 0) reinterpret_cast<float2 *>(to + NT * 16 * DP * 4)[nt * 16 + n16] = make_float2(m[nt], l[nt]);
-            }
-        }
-        __syncthreads();
-        if (wave < step) {
-            const char *from = lds + wave * NT * 16 * (DP * 4 + 8);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float2 ml = reinterpret_cast<const float2 *>(from + NT * 16 * DP * 4)[nt * 16 + n16];
-                const float mn = fmaxf(m[nt], ml.x);
-                const float f0 = m[nt] == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(m[nt] - mn);
-                const float f1 = ml.x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mn);
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[nt][d] = o[nt][d] * f0 + reinterpret_cast<const f32x4 *>(from)[(nt * DB + d) * 64 + lane] * f1;
-                m[nt] = mn;
-                l[nt] = l[nt] * f0 + ml.y * f1;
-            }
-        }
-    }
-    if (wave) return;
-
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = r0 + nt * 16 + n16;
-        if (r >= rows) continue;
-        const RowAt at = row_at(a, pre, b, h, r);
-        if (all_splits > 1) {
-            const int64_t at_part = at.lse * all_splits + part;
-            if (g == 0) a.part_ml[at_part] = make_float2(m[nt], l[nt]);
-            if (k0 == k1) continue;                          // nothing to read for this split
-            float *to = a.part_o + at_part * Dd;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const f32x4 v = ES == 2 ? o[nt][d] : f32x4{o[nt][d / 4 * 4][d % 4], o[nt][d / 4 * 4 + 1][d % 4], o[nt][d / 4 * 4 + 2][d % 4], o[nt][d / 4 * 4 + 3][d % 4]};
-                const int dim = ES == 2 ? 16 * d + 4 * g : 64 * (d / 4) + 16 * g + 4 * (d % 4);
-                if (FULL || dim < Dd) *reinterpret_cast<f32x4 *>(to + dim) = v;
-            }
-            continue;
-        }
-        const bool none = kr.n == 0 || row_pos[nt] < 0;
-        if (a.lse && g == 0) a.lse[at.lse] = none ? NEG_INF : (m[nt] == NEG_INF ? NEG_INF : m[nt] * 0.69314718055994531f) + logf(l[nt]);
-        const float inv = none ? 0.0f : 1.0f / l[nt];
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            f32x4 v = ES == 2 ? o[nt][d] : f32x4{o[nt][d / 4 * 4][d % 4], o[nt][d / 4 * 4 + 1][d % 4], o[nt][d / 4 * 4 + 2][d % 4], o[nt][d / 4 * 4 + 3][d % 4]};
-            const int dim = ES == 2 ? 16 * d + 4 * g : 64 * (d / 4) + 16 * g + 4 * (d % 4);
-            if (!FULL && dim >= Dd) continue;
-            v = none ? f32x4{0, 0, 0, 0} : v * inv;
-            if (ES == 2)
-                *reinterpret_cast<uint2 *>(a.out + at.o + dim * 2) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-            else
-                *reinterpret_cast<f32x4 *>(a.out + at.o + dim * 4) = v;
-        }
-    }
+// A shared prefix for more than 16 rows: its workgroups first, then those of the sequences' own keys, in one launch.
+template <int DP, bool FULL>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
+k_attn_prefix(const AttnArgs a)
+{
+    constexpr int L0 = TilesShape<DP>::LDS, L1 = RowsShape<2, DP, 1>::LDS;
+    __shared__ __align__(16) char lds[L0 > L1 ? L0 : L1];
+    const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
+    if (id < pre_blocks) attn_tiles<DP, FULL>(a, true, id, lds);
+    else attn_rows<2, DP, 1, FULL>(a, false, id - pre_blocks, lds);
 }
 
 // One workgroup a row: its splits' partial results joined in order of the split.  TPR threads hold 4 values each of a row; the 256 / TPR
@@ -412,49 +85,57 @@ k_attn_join(const AttnArgs a)
         *reinterpret_cast<f32x4 *>(to + dim * 4) = o;
 }
 
-template <int ES, int DP>
-void launch_rows(const AttnArgs &a, int nt, hipStream_t stream)
+template <int ES, int DP, int NT>
+void launch_rows(const AttnArgs &a, dim3 grid, hipStream_t stream)
 {
-    const int64_t blocks = (int64_t)a.Hkv * a.pre_tiles * a.pre_splits + (int64_t)a.B * a.Hkv * a.own_tiles * a.splits;
-    const dim3 grid((unsigned int)blocks), block(256);
-    if (nt == 1 && a.D == DP) hipLaunchKernelGGL((k_attn_rows<ES, DP, 1, true>), grid, block, 0, stream, a);
-    else if (nt == 1) hipLaunchKernelGGL((k_attn_rows<ES, DP, 1, false>), grid, block, 0, stream, a);
-    else if (a.D == DP) hipLaunchKernelGGL((k_attn_rows<ES, DP, 2, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((k_attn_rows<ES, DP, 2, false>), grid, block, 0, stream, a);
+    if (a.D == DP) hipLaunchKernelGGL((k_attn_rows<ES, DP, NT, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((k_attn_rows<ES, DP, NT, false>), grid, dim3(256), 0, stream, a);
+}
+
+template <int DP>
+void launch_bf16(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
+{
+    const bool full = a.D == DP;
+    if (path == ATTN_ROWS16) launch_rows<2, DP, 1>(a, grid, stream);
+    else if (path == ATTN_TILES && full) hipLaunchKernelGGL((k_attn_tiles<DP, true>), grid, dim3(256), 0, stream, a);
+    else if (path == ATTN_TILES) hipLaunchKernelGGL((k_attn_tiles<DP, false>), grid, dim3(256), 0, stream, a);
+    else if (full) hipLaunchKernelGGL((k_attn_prefix<DP, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((k_attn_prefix<DP, false>), grid, dim3(256), 0, stream, a);
+}
+
+template <int DP>
+void launch_f32(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
+{
+    if (path == ATTN_ROWS16) launch_rows<4, DP, 1>(a, grid, stream);
+    else launch_rows<4, DP, 2>(a, grid, stream);
 }
 
 }  // namespace
 
-int clada_attn_rows_tile(int rows) { return rows > 16 ? 32 : 16; }
-
-hipError_t clada_attn_rows(const AttnArgs &a, int es, hipStream_t stream)
+hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, hipStream_t stream)
 {
-    const int rows = a.pre_tiles ? a.B * a.G : a.T * a.G;
-    const int nt = clada_attn_rows_tile(rows) / 16;
+    const dim3 grid((unsigned int)((int64_t)a.Hkv * a.pre_tiles * a.pre_splits + (int64_t)a.B * a.Hkv * a.own_tiles * a.splits));
     if (es == 2) {
-        if (a.D <= 64) launch_rows<2, 64>(a, nt, stream);
-        else if (a.D <= 96) launch_rows<2, 96>(a, nt, stream);
-        else if (a.D <= 128) launch_rows<2, 128>(a, nt, stream);
-        else launch_rows<2, 256>(a, nt, stream);
+        if (a.D <= 64) launch_bf16<64>(a, path, grid, stream);
+        else if (a.D <= 96) launch_bf16<96>(a, path, grid, stream);
+        else if (a.D <= 128) launch_bf16<128>(a, path, grid, stream);
+        else launch_bf16<256>(a, path, grid, stream);
     } else {
-        if (a.D <= 64) launch_rows<4, 64>(a, nt, stream);
-        else if (a.D <= 128) launch_rows<4, 128>(a, nt, stream);
-        else launch_rows<4, 256>(a, nt, stream);
+        if (a.D <= 64) launch_f32<64>(a, path, grid, stream);
+        else if (a.D <= 128) launch_f32<128>(a, path, grid, stream);
+        else launch_f32<256>(a, path, grid, stream);
     }
-    return hipGetLastError();
-}
-
-hipError_t clada_attn_join(const AttnArgs &a, int es, hipStream_t stream)
-{
-    const dim3 grid((unsigned int)((int64_t)a.B * a.T * a.Hq)), block(256);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits + a.pre_splits == 1) return e;
+    const dim3 rows((unsigned int)((int64_t)a.B * a.T * a.Hq)), block(256);
     if (es == 2) {
-        if (a.D <= 64) hipLaunchKernelGGL((k_attn_join<2, 16>), grid, block, 0, stream, a);
-        else if (a.D <= 128) hipLaunchKernelGGL((k_attn_join<2, 32>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_attn_join<2, 64>), grid, block, 0, stream, a);
+        if (a.D <= 64) hipLaunchKernelGGL((k_attn_join<2, 16>), rows, block, 0, stream, a);
+        else if (a.D <= 128) hipLaunchKernelGGL((k_attn_join<2, 32>), rows, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_attn_join<2, 64>), rows, block, 0, stream, a);
     } else {
-        if (a.D <= 64) hipLaunchKernelGGL((k_attn_join<4, 16>), grid, block, 0, stream, a);
-        else if (a.D <= 128) hipLaunchKernelGGL((k_attn_join<4, 32>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_attn_join<4, 64>), grid, block, 0, stream, a);
+        if (a.D <= 64) hipLaunchKernelGGL((k_attn_join<4, 16>), rows, block, 0, stream, a);
+        else if (a.D <= 128) hipLaunchKernelGGL((k_attn_join<4, 32>), rows, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_attn_join<4, 64>), rows, block, 0, stream, a);
     }
     return hipGetLastError();
 }

@@ -137,8 +137,8 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     a.window = window;
     a.sinks = window ? sinks : 0;
     const int es = (int)dtype_size(cache->dtype);
-    const bool many = es == 2 && T * a.G >= 64;
-    const int tile = many ? 128 : clada_attn_rows_tile(T * a.G);
+    const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS16 : es == 2 ? ATTN_TILES : ATTN_ROWS32;
+    const int tile = path == ATTN_ROWS16 ? 16 : path == ATTN_ROWS32 ? 32 : 128;
     a.own_tiles = (T * a.G + tile - 1) / tile;
     const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
     int64_t keys = cache->capacity;                          // what a tile can see at most
@@ -149,8 +149,7 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     a.splits = splits_for(units, keys, ctx->num_cu);
     if (units * a.splits > INT32_MAX) return clada_fail(ctx, CLADA_ERR_SHAPE, "the call has too many rows");
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
-    CLADA_CHECK_HIP(ctx, many ? clada_attn_tiles(a, (hipStream_t)hip_stream) : clada_attn_rows(a, es, (hipStream_t)hip_stream));
-    if (a.splits > 1) CLADA_CHECK_HIP(ctx, clada_attn_join(a, es, (hipStream_t)hip_stream));
+    CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
     return CLADA_OK;
 }
 
@@ -177,14 +176,15 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     fill(a, q, out, cache, lens, B, 1, Hq, scale, lse);
     a.pre = kv_of(prefix);
     a.pre_n = prefix_len;
-    const int es = (int)dtype_size(cache->dtype), tile = clada_attn_rows_tile(B * a.G);
+    const int es = (int)dtype_size(cache->dtype);
+    const AttnPath path = B * a.G <= 16 ? ATTN_ROWS16 : es == 2 ? ATTN_PREFIX : ATTN_ROWS32;
+    const int tile = path == ATTN_ROWS16 ? 16 : path == ATTN_ROWS32 ? 32 : 128, own = path == ATTN_ROWS32 ? 32 : 16;
     a.pre_tiles = (B * a.G + tile - 1) / tile;
-    a.own_tiles = (a.G + tile - 1) / tile;
+    a.own_tiles = (a.G + own - 1) / own;
     a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
     a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
     if ((st = place_parts(ctx, a)) != CLADA_OK) return st;
-    CLADA_CHECK_HIP(ctx, clada_attn_rows(a, es, (hipStream_t)hip_stream));
-    CLADA_CHECK_HIP(ctx, clada_attn_join(a, es, (hipStream_t)hip_stream));
+    CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
     return CLADA_OK;
 }
 

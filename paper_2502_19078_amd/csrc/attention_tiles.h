@@ -1,6 +1,6 @@
-// bf16 attention for many rows: prompts, long chunks, and a shared prefix read for a large batch.
+// The many-row body of the attention kernels, bf16 (attention.hip): prompts, chunks, and a shared prefix read for a batch.
 //
-// The same sums as in attention.hip, bound by the matrix cores and the vector units: a tile of 32 rows by 64 keys is 32 products of
+// The same sums as in attention_rows.h, bound by the matrix cores and the vector units: a tile of 32 rows by 64 keys is 32 products of
 // 32x32x16 (1024 clocks of a SIMD at 128 values a head) beside 32 exponentials, maxima, sums and conversions a lane (about as many clocks
 // again).  A workgroup of four waves takes 128 rows, 32 a wave; K and V tiles of 64 keys go through registers into one of two LDS buffers while
 // the other is multiplied, one barrier a tile.  Two workgroups share a compute unit, so one's products run under the other's exponentials.
@@ -8,13 +8,10 @@
 // Scores are formed transposed (S^T = K Q^T): a lane holds scores of one row only, keys 8 (i / 4) + 4 (lane / 32) + i % 4 of each 32, and the same
 // registers, rounded to bf16, are the second operand of O^T = V^T P^T when its keys are counted in that order (V is turned by
 // ds_read_tr16).  The weights' rounding (2^-8 at most, to nearest) is of the size of the output's own; their sum is taken before it.
-#include <math.h>
-
+#pragma once
 #include "attention.h"
 
 namespace {
-
-constexpr float NEG_INF = -INFINITY;
 
 // Orders the LDS accesses around it; leaves loads from memory in flight.
 __device__ __forceinline__ void tile_barrier()
@@ -24,17 +21,21 @@ __device__ __forceinline__ void tile_barrier()
     asm volatile("" ::: "memory");
 }
 
+template <int DP>
+struct TilesShape {
+    static constexpr int KT = DP <= 128 ? 64 : 32;           // keys of a tile
+    static constexpr int KP = DP * 2 + 16, VP = DP * 2 + 32; // row pitches: K rows 4 banks apart, V rows 8
+    static constexpr int BUF = KT * (KP + VP), LDS = 2 * BUF;
+};
+
 template <int DP, bool FULL>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
-k_attn_tiles(const AttnArgs a)
+__device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, const int id, char *lds)
 {
-    constexpr int KT = DP <= 128 ? 64 : 32, KB = KT / 32;    // keys of a tile
+    using S = TilesShape<DP>;
+    constexpr int KT = S::KT, KB = KT / 32, KP = S::KP, VP = S::VP, BUF = S::BUF;
     constexpr int KD = DP / 16, DB = DP / 32;
     constexpr int CPR = DP / 8, ROWS = KT * CPR / 256;       // 16-byte chunks of a row; chunks of K (and of V) a thread stages
-    constexpr int KP = DP * 2 + 16, VP = DP * 2 + 32;        // row pitches: K rows 4 banks apart, V rows 8
-    constexpr int BUF = KT * (KP + VP);
     static_assert(KT * CPR % 256 == 0, "whole passes");
-    __shared__ __align__(16) char lds[2 * BUF];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, hh = lane >> 5, t16 = lane & 15, g = lane >> 4;
@@ -42,9 +43,8 @@ k_attn_tiles(const AttnArgs a)
 
     // Units (sequence, key head) fastest: consecutive workgroups go to different XCDs, so a unit's tiles share an L2.  The last row tiles see the
     // most keys and come first.
-    const bool pre = a.pre_tiles != 0;
     const int units = pre ? a.Hkv : a.B * a.Hkv, tiles = pre ? a.pre_tiles : a.own_tiles, splits = pre ? a.pre_splits : a.splits;
-    const int unit = blockIdx.x % units, rest = blockIdx.x / units;
+    const int unit = id % units, rest = id / units;
     const int split = rest % splits, tile = tiles - 1 - rest / splits;
     const int h = unit % a.Hkv, b = unit / a.Hkv;
     const int rows = (pre ? a.B : a.T) * a.G, r0 = tile * 128;
@@ -70,6 +70,7 @@ k_attn_tiles(const AttnArgs a)
     const RowAt at = row_at(a, pre, b, h, rc);
     const int row_pos = pre ? a.pre_n : rc / a.G < qlen ? first_pos + rc / a.G : -1;
     // positions of the wave's first and last row, for tiles that all or none of its rows see
+    const bool idle = r0 + wave * 32 >= rows;
     const int wr0 = min(r0 + wave * 32, rows - 1), wr1 = min(r0 + wave * 32 + 31, rows - 1);
     const int wave_a = pre ? a.pre_n : wr0 / a.G < qlen ? first_pos + wr0 / a.G : -1;
     const int wave_b = pre ? a.pre_n : min(wr1 / a.G, qlen - 1) + first_pos;
@@ -92,7 +93,7 @@ k_attn_tiles(const AttnArgs a)
     auto fetch = [&](int i) {
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
-            const int id = tid + 256 * j, key = i + id / CPR, col = id % CPR * 16;
+            const int c = tid + 256 * j, key = i + c / CPR, col = c % CPR * 16;
             const bool in = FULL || col < Dd * 2;
             const int64_t off = kr.row(kr.pos(min(key, k1 - 1)), kv) * kv.sn + (in ? col : 0);
             sk[j] = *reinterpret_cast<const u32x4 *>(kp + off);
@@ -105,7 +106,7 @@ k_attn_tiles(const AttnArgs a)
         char *to = lds + buf * BUF;
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
-            const int id = tid + 256 * j, key = id / CPR, col = id % CPR * 16;
+            const int c = tid + 256 * j, key = c / CPR, col = c % CPR * 16;
             *reinterpret_cast<u32x4 *>(to + key * KP + col) = sk[j];
             *reinterpret_cast<u32x4 *>(to + KT * KP + key * VP + col) = sv[j];
         }
@@ -138,7 +139,7 @@ k_attn_tiles(const AttnArgs a)
         for (int i = k0; i < k1; i += KT, buf ^= 1) {
             const int last = min(i + KT, k1) - 1, p_first = kr.pos(i), p_last = kr.pos(last);
             // (a tile that begins among the sinks is looked at key by key)
-            const bool none = p_first > wave_b || (a.window && p_first >= a.sinks && p_last <= wave_a - a.window && wave_a >= 0);
+            const bool none = idle || p_first > wave_b || (a.window && p_first >= a.sinks && p_last <= wave_a - a.window && wave_a >= 0);
             const bool all = last == i + KT - 1 && !ragged && (pre || (p_last <= wave_a && (a.window == 0 || p_first > wave_b - a.window || p_last < a.sinks)));
             if (!none) {
                 const char *kb = lds + buf * BUF, *vb = kb + KT * KP;
@@ -270,22 +271,4 @@ k_attn_tiles(const AttnArgs a)
         }
 }
 
-template <int DP>
-void launch_tiles(const AttnArgs &a, hipStream_t stream)
-{
-    const int64_t blocks = a.pre_tiles ? (int64_t)a.Hkv * a.pre_tiles * a.pre_splits : (int64_t)a.B * a.Hkv * a.own_tiles * a.splits;
-    const dim3 grid((unsigned int)blocks), block(256);
-    if (a.D == DP) hipLaunchKernelGGL((k_attn_tiles<DP, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((k_attn_tiles<DP, false>), grid, block, 0, stream, a);
-}
-
 }  // namespace
-
-hipError_t clada_attn_tiles(const AttnArgs &a, hipStream_t stream)
-{
-    if (a.D <= 64) launch_tiles<64>(a, stream);
-    else if (a.D <= 96) launch_tiles<96>(a, stream);
-    else if (a.D <= 128) launch_tiles<128>(a, stream);
-    else launch_tiles<256>(a, stream);
-    return hipGetLastError();
-}
