@@ -9,6 +9,8 @@
 // registers, rounded to bf16, are the second operand of O^T = V^T P^T when its keys are counted in that order (V is turned by
 // ds_read_tr16).  The weights' rounding (2^-8 at most, to nearest) is of the size of the output's own; their sum is taken before it.
 #pragma once
+#include <type_traits>
+
 #include "attention.h"
 
 namespace {
@@ -34,8 +36,9 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     using S = TilesShape<DP>;
     constexpr int KT = S::KT, KB = KT / 32, KP = S::KP, VP = S::VP, BUF = S::BUF;
     constexpr int KD = DP / 16, DB = DP / 32;
-    constexpr int CPR = DP / 8, ROWS = KT * CPR / 256;       // 16-byte chunks of a row; chunks of K (and of V) a thread stages
-    static_assert(KT * CPR % 256 == 0, "whole passes");
+    constexpr int CPR = DP == 96 ? 16 : DP / 8, ROWS = KT * CPR / 256;      // threads a row, 16 bytes each; rows of K (and of V) a thread stages
+    constexpr bool WHOLE = FULL && CPR * 8 == DP;            // every thread has a chunk of the row
+    static_assert(KT * CPR % 256 == 0 && 256 % CPR == 0, "whole passes");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, hh = lane >> 5, t16 = lane & 15, g = lane >> 4;
@@ -89,24 +92,41 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     }
 
     const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
+    const int first_key = tid / CPR, col = tid % CPR * 16;   // of the chunks that this thread stages: keys first_key + j * (256 / CPR)
+    const bool in = WHOLE || col < Dd * 2;
+    const unsigned int lane_off = (unsigned int)first_key * (unsigned int)kv.sn + (in ? col : 0), step_off = 256 / CPR * (unsigned int)kv.sn;
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
     auto fetch = [&](int i) {
+        // A whole tile of consecutive cache rows has one base for all lanes (offsets in 32 bits: no row further than 32 MiB from the next)
+        const int64_t row0 = kr.row(kr.pos(i), kv);
+        if (i + KT <= k1 && kv.sn < (1 << 25) && kr.row(kr.pos(i + KT - 1), kv) - row0 == KT - 1) {
+            const char *kt = kp + row0 * kv.sn, *vt = vp + row0 * kv.sn;
 #pragma unroll
-        for (int j = 0; j < ROWS; ++j) {
-            const int c = tid + 256 * j, key = i + c / CPR, col = c % CPR * 16;
-            const bool in = FULL || col < Dd * 2;
-            const int64_t off = kr.row(kr.pos(min(key, k1 - 1)), kv) * kv.sn + (in ? col : 0);
-            sk[j] = *reinterpret_cast<const u32x4 *>(kp + off);
-            sv[j] = *reinterpret_cast<const u32x4 *>(vp + off);
-            if (!in) sk[j] = u32x4{0, 0, 0, 0};
-            if (!in || key >= k1) sv[j] = u32x4{0, 0, 0, 0};
+            for (int j = 0; j < ROWS; ++j) {
+                sk[j] = *reinterpret_cast<const u32x4 *>(kt + (lane_off + j * step_off));
+                sv[j] = *reinterpret_cast<const u32x4 *>(vt + (lane_off + j * step_off));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < ROWS; ++j) {
+                const int key = i + first_key + j * (256 / CPR);
+                const int64_t off = kr.row(kr.pos(min(key, k1 - 1)), kv) * kv.sn + (in ? col : 0);
+                sk[j] = *reinterpret_cast<const u32x4 *>(kp + off);
+                sv[j] = *reinterpret_cast<const u32x4 *>(vp + off);
+                if (key >= k1) sv[j] = u32x4{0, 0, 0, 0};
+            }
+        }
+        if (!WHOLE && !in) {
+#pragma unroll
+            for (int j = 0; j < ROWS; ++j) sk[j] = sv[j] = u32x4{0, 0, 0, 0};
         }
     };
     auto put = [&](int buf) {
         char *to = lds + buf * BUF;
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
-            const int c = tid + 256 * j, key = c / CPR, col = c % CPR * 16;
+            const int key = first_key + j * (256 / CPR);
+            if (CPR * 8 != DP && col >= DP * 2) continue;
             *reinterpret_cast<u32x4 *>(to + key * KP + col) = sk[j];
             *reinterpret_cast<u32x4 *>(to + KT * KP + key * VP + col) = sv[j];
         }
@@ -115,7 +135,8 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     f32x16 o[DB];
     float m, l;
     unsigned int up[DB], down[DB];                           // halfwords of a bit for every output
-    for (int pass = PASS_PLAIN; pass <= PASS_REST; ++pass) {
+    auto walk = [&](auto plain, int pass) {
+        constexpr bool PLAIN = decltype(plain)::value;
         m = NEG_INF;
         l = 0.0f;
 #pragma unroll
@@ -123,7 +144,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
         auto shape = [&]() {
-            if (pass) {
+            if (!PLAIN) {
 #pragma unroll
                 for (int j = 0; j < ROWS; ++j) values_for_pass<2>(sv[j], pass);
             }
@@ -154,7 +175,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                         s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), s[k], 0, 0, 0);
                     }
                 }
-                if (pass == PASS_UP || pass == PASS_DOWN) {
+                if (!PLAIN && pass != PASS_REST) {
 #pragma unroll
                     for (int k = 0; k < KB; ++k)
 #pragma unroll
@@ -215,26 +236,28 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             }
             tile_barrier();
         }
-        if (pass == PASS_PLAIN) {
-            bool fine = true;
+    };
+    walk(std::true_type{}, PASS_PLAIN);
+    bool fine = true;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) fine = fine && fabsf(o[d][e]) < INFINITY;
-            if (!__syncthreads_or(!fine)) break;
-            continue;
-        }
+        for (int e = 0; e < 16; ++e) fine = fine && fabsf(o[d][e]) < INFINITY;
+    if (__syncthreads_or(!fine)) {
+        for (int pass = PASS_UP; pass <= PASS_REST; ++pass) {
+            walk(std::false_type{}, pass);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            if (pass == PASS_UP) up[d] = 0;
-            if (pass == PASS_DOWN) down[d] = 0;
+            for (int d = 0; d < DB; ++d) {
+                if (pass == PASS_UP) up[d] = 0;
+                if (pass == PASS_DOWN) down[d] = 0;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (pass == PASS_UP) up[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
-                else if (pass == PASS_DOWN) down[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
-                else {
-                    if (up[d] >> e & 1) o[d][e] += INFINITY;
-                    if (down[d] >> e & 1) o[d][e] -= INFINITY;
+                for (int e = 0; e < 16; ++e) {
+                    if (pass == PASS_UP) up[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
+                    else if (pass == PASS_DOWN) down[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
+                    else {
+                        if (up[d] >> e & 1) o[d][e] += INFINITY;
+                        if (down[d] >> e & 1) o[d][e] -= INFINITY;
+                    }
                 }
             }
         }
