@@ -10,6 +10,7 @@
 // ds_read_tr16).  The weights' rounding (2^-8 at most, to nearest) is of the size of the output's own; their sum is taken before it.
 #pragma once
 #include <type_traits>
+#include <utility>
 
 #include "attention.h"
 
@@ -22,6 +23,12 @@ __device__ __forceinline__ void tile_barrier()
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+
+// f(0) .. f(N - 1) with the index as a constant.
+template <class F, int... I>
+__device__ __forceinline__ void unrolled_(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F &&f) { unrolled_(f, std::make_integer_sequence<int, N>{}); }
 
 template <int DP>
 struct TilesShape {
@@ -166,15 +173,26 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                 const char *kb = lds + buf * BUF, *vb = kb + KT * KP;
                 f32x16 s[KB];
 #pragma unroll
-                for (int k = 0; k < KB; ++k) {
+                for (int k = 0; k < KB; ++k)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[k][e] = 0.0f;
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int c = 0; c < KD; ++c) {
+                for (int c = 0; c < KD; ++c)
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) {
                         const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
                         s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), s[k], 0, 0, 0);
                     }
+                // six fragments ahead of the products
+                __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+                for (int x = 0; x < KD * KB - 6; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
+                __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+                __builtin_amdgcn_sched_barrier(0);
                 if (!PLAIN && pass != PASS_REST) {
 #pragma unroll
                     for (int k = 0; k < KB; ++k)
@@ -207,27 +225,42 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                     for (int d = 0; d < DB; ++d) o[d] *= f;
                 }
                 const float base = m == NEG_INF ? 0.0f : m;
-                unsigned int pk[KB][8];
+                // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and
+                // the reads of V four products ahead.
+                constexpr int STEPS = 2 * KB, AHEAD = 4;
+                u32x4 vt[AHEAD], pk[2];
+                auto weight = [&](auto step, int e) {        // the e-th of the step's eight weights of this lane
+                    constexpr int st = decltype(step)::value, k = st / 2, c = st % 2;
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[k][8 * c + e], scale2, -base));
+                    l += p;
+                    s[k][8 * c + e] = p;
+                    if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
+                };
+                const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
+                auto read_v = [&](int x) {
+                    const char *from = src + x / DB * 16 * VP + x % DB * 64;
+                    const uint2 u0 = read_tr16(from), u1 = read_tr16(from + 8 * VP);
+                    vt[x % AHEAD] = u32x4{u0.x, u0.y, u1.x, u1.y};
+                };
 #pragma unroll
-                for (int k = 0; k < KB; ++k)
+                for (int x = 0; x < AHEAD; ++x) read_v(x);
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[k][e], scale2, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[k][e + 1], scale2, -base));
-                        l += p0 + p1;
-                        pk[k][e >> 1] = pack_bf16(p0, p1);
-                    }
+                for (int e = 0; e < 8; ++e) weight(std::integral_constant<int, 0>{}, e);
+                unrolled<STEPS>([&](auto step) {
+                    constexpr int st = decltype(step)::value;
 #pragma unroll
-                for (int k = 0; k < KB; ++k)
+                    for (int d = 0; d < DB; ++d) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        const int x = st * DB + d;
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, pk[st & 1]), o[d], 0, 0, 0);
+                        if (x + AHEAD < STEPS * DB) read_v(x + AHEAD);
+                        if constexpr (st + 1 < STEPS) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pk[k][4 * c], pk[k][4 * c + 1], pk[k][4 * c + 2], pk[k][4 * c + 3]});
-                        const char *src = vb + (k * 32 + c * 16 + 4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) {
-                            const uint2 u0 = read_tr16(src + d * 64), u1 = read_tr16(src + d * 64 + 8 * VP);
-                            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y}), pf, o[d], 0, 0, 0);
+                            for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) weight(std::integral_constant<int, st + 1>{}, e);
                         }
                     }
+                });
+                __builtin_amdgcn_sched_barrier(0);
             }
             if (i + KT < k1) {
                 shape();
