@@ -39,6 +39,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr float NEG_INF = -__builtin_inff();
 
@@ -62,34 +63,6 @@ __device__ __forceinline__ RowAt row_at(const AttnArgs &a, bool pre, int b, int 
 __device__ __forceinline__ uint2 read_tr16(const char *p)
 {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)p));
-}
-
-// Values that are not finite.  A weight of zero times such a value is no zero, so a product over a tile would hand it to rows that do not see
-// its key.  A pass whose outputs are not all finite is therefore followed by three more over the same keys: the weights 1 for every
-// key that a row sees, and V with 1 where a value is +inf or NaN (PASS_UP), then -inf or NaN (PASS_DOWN), which count such values for each
-// output; then the plain weights with those values taken out (PASS_REST).  An output with a count is that infinity, or NaN with both.
-enum { PASS_PLAIN = 0, PASS_UP = 1, PASS_DOWN = 2, PASS_REST = 3 };
-template <int ES>
-__device__ __forceinline__ void values_for_pass(u32x4 &v, int pass)
-{
-    if (pass == PASS_PLAIN) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const unsigned int w = v[e];
-        if (ES == 4) {
-            const bool odd = (w & 0x7f800000u) == 0x7f800000u, counts = odd && (w << 9 || (w >> 31) == (unsigned int)(pass == PASS_DOWN));
-            v[e] = pass == PASS_REST ? (odd ? 0u : w) : (counts ? 0x3f800000u : 0u);
-        } else {
-            unsigned int r = 0;
-#pragma unroll
-            for (int s = 0; s < 32; s += 16) {
-                const unsigned int x = w >> s & 0xffffu;
-                const bool odd = (x & 0x7f80u) == 0x7f80u, counts = odd && ((x & 0x7fu) || (x >> 15) == (unsigned int)(pass == PASS_DOWN));
-                r |= (pass == PASS_REST ? (odd ? 0u : x) : (counts ? 0x3f80u : 0u)) << s;
-            }
-            v[e] = r;
-        }
-    }
 }
 
 // The keys that a tile's rows may see, in order: `head` sinks from position 0 on, then the positions from `lo` on.
@@ -123,11 +96,92 @@ __device__ __forceinline__ KeyRange key_range(const AttnKV &kv, int first_pos, i
     return k;
 }
 
+// Which of the keys base, base + 1, ... of a range, up to `end`, the row at position row_pos sees: comparisons of small constants with a few
+// numbers.  Keys below kr.head are sinks that all rows of the range see (rows at negative positions see nothing, whatever this says).
+struct Sight {
+    int end, head, causal, recent, sink;
+    __device__ __forceinline__ bool operator()(int c) const
+    {
+        return (c < end) & ((c < head) | ((c <= causal) & ((c > recent) | (c < sink))));
+    }
+};
+__device__ __forceinline__ Sight sight(const KeyRange &kr, int base, int end, int row_pos, int window, int sinks)
+{
+    const int p0 = kr.lo - kr.head + base;                   // position of key `base` if it is no sink
+    return {end - base, kr.head - base, row_pos - p0, window ? row_pos - window - p0 : INT32_MIN, sinks - p0};
+}
+
 // Tokens that a sequence holds and queries that the call brings for it, whatever the arrays say.
 __device__ __forceinline__ void sequence_lens(const AttnArgs &a, int b, int &len, int &qlen)
 {
     len = max(a.lens[b], 0);
     if (a.kv.ring == 0) len = min(len, a.kv.capacity);
     qlen = a.q_lens ? min(max(a.q_lens[b], 0), a.T) : a.T;
+}
+
+// A product over a tile gives every row every key of it, and a weight of zero (or the lower half of a weight) times a value that is not finite
+// is no zero.  A row whose outputs are not finite is therefore computed a second time by one wave, key by key as it sees them: 64 keys'
+// scores at once, a lane each, then their values one after the other, a lane for every 64th dimension.  It also serves a row whose weights
+// have outgrown fp32.  A row whose sum is NaN stays: a NaN score makes every output NaN.
+struct RowAgain { float m, l, o[CLADA_ATTN_MAX_D / 64]; };
+
+template <int ES>
+__device__ __forceinline__ float attn_value(const char *row, int d)
+{
+    return ES == 2 ? __uint_as_float((unsigned int)reinterpret_cast<const unsigned short *>(row)[d] << 16) : reinterpret_cast<const float *>(row)[d];
+}
+
+template <int ES>
+__device__ __forceinline__ RowAgain attn_row_again(const AttnArgs &a, const KeyRange &kr, const AttnKV &kv, const char *kp, const char *vp, const char *q,
+                                                   int row_pos, int k0, int k1)
+{
+    const int lane = threadIdx.x & 63;
+    RowAgain r;
+    r.m = NEG_INF;
+    r.l = 0.0f;
+    for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j) r.o[j] = 0.0f;
+    for (int base = k0; base < k1; base += 64) {
+        const int key = base + lane, p = kr.pos(min(key, k1 - 1));
+        const bool see = key < k1 && p <= row_pos && (a.window == 0 || p > row_pos - a.window || p < a.sinks);
+        const int64_t off = kr.row(p, kv) * kv.sn;
+        float x = NEG_INF;
+        if (see) {
+            float s = 0.0f;
+            for (int d = 0; d < a.D; ++d) s = fmaf(attn_value<ES>(kp + off, d), attn_value<ES>(q, d), s);
+            x = s * a.scale2;
+        }
+        const float mn = fmaxf(r.m, wave_max(x)), f = r.m == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(r.m - mn);
+        const float w = see ? __builtin_amdgcn_exp2f(x - (mn == NEG_INF ? 0.0f : mn)) : 0.0f;
+        r.l = r.l * f + wave_sum(w);
+        for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j)
+            if (r.m != NEG_INF) r.o[j] *= f;
+        r.m = mn;
+        for (unsigned long long left = __ballot(see); left; left &= left - 1) {
+            const int t = __builtin_ctzll(left);
+            const float wt = __shfl(w, t);
+            const int64_t row = __shfl(off, t);
+            for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j)
+                if (lane + 64 * j < a.D) r.o[j] = fmaf(wt, attn_value<ES>(vp + row, lane + 64 * j), r.o[j]);
+        }
+    }
+    return r;
+}
+
+// What a row of a split, or of a call without splits, leaves behind: by a wave that holds it as above.
+template <int ES>
+__device__ __forceinline__ void attn_store_again(const AttnArgs &a, const RowAgain &r, const RowAt &at, int part)
+{
+    const int lane = threadIdx.x & 63, splits = a.splits + a.pre_splits;
+    if (splits > 1) {
+        if (lane == 0) a.part_ml[at.lse * splits + part] = make_float2(r.m, r.l);
+    } else if (a.lse && lane == 0)
+        a.lse[at.lse] = r.m * 0.69314718055994531f + logf(r.l);
+    for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j) {
+        const int d = lane + 64 * j;
+        if (d >= a.D) continue;
+        if (splits > 1) a.part_o[(at.lse * splits + part) * a.D + d] = r.o[j];
+        else if (ES == 2) reinterpret_cast<unsigned short *>(a.out + at.o)[d] = (unsigned short)f32_to_bf16_bits(r.o[j] / r.l);
+        else reinterpret_cast<float *>(a.out + at.o)[d] = r.o[j] / r.l;
+    }
 }
 #endif

@@ -26,7 +26,7 @@ struct RowsShape {
 };
 
 template <int ES, int DP, int NT, bool FULL>
-__device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int id, char *lds)
+__device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, const int block, char *lds)
 {
     using S = RowsShape<ES, DP, NT>;
     constexpr int CH = DP * ES / 64;                         // chunks of 64 bytes in a row: lane group g holds 16 bytes of each
@@ -40,7 +40,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int
     const int Dd = FULL ? DP : a.D;
 
     // which tile of which keys
-    int split, b = 0, h, tile, splits, rows;
+    int id = block, split, b = 0, h, tile, splits, rows;
     if (pre) {
         split = id % a.pre_splits;
         id /= a.pre_splits;
@@ -135,8 +135,6 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int
         }
     };
 
-    unsigned int up[NT][(4 * DB + 31) / 32], down[NT][(4 * DB + 31) / 32];     // a bit for every output
-    for (int pass = PASS_PLAIN; pass <= PASS_REST; ++pass) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt] = NEG_INF;
@@ -169,10 +167,6 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int
             }
         const int p_first = kr.pos(i), p_last = kr.pos(min(i + KS, k1) - 1);
         const bool mixed = !one_pos && !(p_last <= kr.pos_a && (a.window == 0 || p_first > kr.pos_b - a.window || p_last < a.sinks));
-        if (pass) {
-#pragma unroll
-            for (int j = 0; j < VL; ++j) values_for_pass<ES>(vf[j], pass);
-        }
         if (ES == 2) {
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
@@ -191,18 +185,15 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float top = NEG_INF;
+            const Sight see = sight(kr, i + 4 * g, k1, row_pos[nt], a.window, a.sinks);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int key = i + kb * 16 + 4 * g + e;
-                    float x = pass == PASS_UP || pass == PASS_DOWN ? 0.0f : s[nt][kb][e] * a.scale2;
-                    bool see = key < k1;
-                    if (mixed) {
-                        const int p = kr.pos(key);
-                        see = see && p <= row_pos[nt] && (a.window == 0 || p > row_pos[nt] - a.window || p < a.sinks);
-                    }
-                    x = see ? x : NEG_INF;
+                    const int key = kb * 16 + e;
+                    float x = s[nt][kb][e] * a.scale2;
+                    const bool seen = mixed ? see(key) : key < see.end;
+                    x = seen ? x : NEG_INF;
                     s[nt][kb][e] = x;
                     top = fmaxf(top, x);
                 }
@@ -261,34 +252,6 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int
                     }
         }
     }
-    if (pass == PASS_PLAIN) {
-        bool fine = true;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) fine = fine && fabsf(o[nt][d][e]) < INFINITY;
-        if (__all(fine)) break;
-        continue;
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int w = (4 * d + e) / 32, bit = (4 * d + e) % 32;
-                if (bit == 0 && pass == PASS_UP) up[nt][w] = 0;
-                if (bit == 0 && pass == PASS_DOWN) down[nt][w] = 0;
-                if (pass == PASS_UP) up[nt][w] |= (o[nt][d][e] > 0.0f ? 1u : 0u) << bit;
-                else if (pass == PASS_DOWN) down[nt][w] |= (o[nt][d][e] > 0.0f ? 1u : 0u) << bit;
-                else {
-                    if (up[nt][w] >> bit & 1) o[nt][d][e] += INFINITY;
-                    if (down[nt][w] >> bit & 1) o[nt][d][e] -= INFINITY;
-                }
-            }
-    }
 
     // join the waves: 2 and 3 hand over to 0 and 1, then 1 to 0
 #pragma unroll
@@ -324,12 +287,40 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, int
             }
         }
     }
+    // rows that are not finite, bit for row, from wave 0 to all
+    __syncthreads();
+    unsigned int *s_again = reinterpret_cast<unsigned int *>(lds);
+    if (wave == 0) {
+        unsigned int again = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            bool fine = l[nt] < INFINITY;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) fine = fine && fabsf(o[nt][d][e]) < INFINITY;
+            unsigned long long odd = __ballot(!fine && !(l[nt] != l[nt]) && row_pos[nt] >= 0 && r0 + nt * 16 + n16 < rows);
+            odd |= odd >> 32;
+            again |= (unsigned int)((odd | odd >> 16) & 0xffff) << (nt * 16);
+        }
+        if (lane == 0) *s_again = again;
+    }
+    __syncthreads();
+    const unsigned int again = kr.n ? __builtin_amdgcn_readfirstlane(*s_again) : 0u;
+    if (again) {
+        for (int t = wave; t < 16 * NT; t += 4) {
+            if (!(again >> t & 1)) continue;
+            const int r = r0 + t;
+            const RowAt at = row_at(a, pre, b, h, r);
+            attn_store_again<ES>(a, attn_row_again<ES>(a, kr, kv, kp, vp, a.q + at.q, pre || a.pre_splits ? INT32_MAX : first_pos + r / a.G, k0, k1), at, part);
+        }
+    }
     if (wave) return;
 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int r = r0 + nt * 16 + n16;
-        if (r >= rows) continue;
+        if (r >= rows || (again >> (nt * 16 + n16) & 1)) continue;
         const RowAt at = row_at(a, pre, b, h, r);
         if (all_splits > 1) {
             const int64_t at_part = at.lse * all_splits + part;

@@ -77,7 +77,6 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 
     // this lane's row
     const int r = r0 + wave * 32 + n32, rc = min(r, rows - 1);
-    const RowAt at = row_at(a, pre, b, h, rc);
     const int row_pos = pre ? a.pre_n : rc / a.G < qlen ? first_pos + rc / a.G : -1;
     // positions of the wave's first and last row, for tiles that all or none of its rows see
     const bool idle = r0 + wave * 32 >= rows;
@@ -93,7 +92,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     for (int c = 0; c < KD; ++c) {
         const int off = 32 * c + 16 * hh;
         const bool in = FULL || off < Dd * 2;
-        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + at.q + (in ? off : 0));
+        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + row_at(a, pre, b, h, rc).q + (in ? off : 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) qf[c][e] = in ? qf[c][e] ^ flip : 0u;
     }
@@ -128,37 +127,30 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             for (int j = 0; j < ROWS; ++j) sk[j] = sv[j] = u32x4{0, 0, 0, 0};
         }
     };
+    const unsigned int put_k = first_key * KP + col, put_v = KT * KP + first_key * VP + col;
     auto put = [&](int buf) {
-        char *to = lds + buf * BUF;
+        if (CPR * 8 != DP && col >= DP * 2) return;
+        char *to_k = lds + (put_k + buf * BUF), *to_v = lds + (put_v + buf * BUF);
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
-            const int key = first_key + j * (256 / CPR);
-            if (CPR * 8 != DP && col >= DP * 2) continue;
-            *reinterpret_cast<u32x4 *>(to + key * KP + col) = sk[j];
-            *reinterpret_cast<u32x4 *>(to + KT * KP + key * VP + col) = sv[j];
+            *reinterpret_cast<u32x4 *>(to_k + j * (256 / CPR) * KP) = sk[j];
+            *reinterpret_cast<u32x4 *>(to_v + j * (256 / CPR) * VP) = sv[j];
         }
     };
 
+    // A row's maximum is that of the first tile that it sees; its weights grow past 1 from there on (as floats they lose nothing) and are
+    // scaled down where a sum passes 2^60: no maxima in the loop.  Where scores rise by more than 60 powers of two within a tile, the row's
+    // sums overflow and it is computed again below.
     f32x16 o[DB];
     float m, l;
-    unsigned int up[DB], down[DB];                           // halfwords of a bit for every output
-    auto walk = [&](auto plain, int pass) {
-        constexpr bool PLAIN = decltype(plain)::value;
-        m = NEG_INF;
+        m = row_pos < 0 || r >= rows ? 0.0f : NEG_INF;       // (a row that sees nothing does not wait for its first key)
         l = 0.0f;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
-        auto shape = [&]() {
-            if (!PLAIN) {
-#pragma unroll
-                for (int j = 0; j < ROWS; ++j) values_for_pass<2>(sv[j], pass);
-            }
-        };
         if (k0 < k1) {
             fetch(k0);
-            shape();
             put(0);
             if (k0 + KT < k1) fetch(k0 + KT);
         }
@@ -172,17 +164,13 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             if (!none) {
                 const char *kb = lds + buf * BUF, *vb = kb + KT * KP;
                 f32x16 s[KB];
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[k][e] = 0.0f;
-                __builtin_amdgcn_sched_barrier(0);
+                const f32x16 zero = {};
 #pragma unroll
                 for (int c = 0; c < KD; ++c)
 #pragma unroll
                     for (int k = 0; k < KB; ++k) {
                         const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
-                        s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), s[k], 0, 0, 0);
+                        s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
                     }
                 // six fragments ahead of the products
                 __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
@@ -193,36 +181,28 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                 }
                 __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                if (!PLAIN && pass != PASS_REST) {
-#pragma unroll
-                    for (int k = 0; k < KB; ++k)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[k][e] = 0.0f;
-                }
                 if (!all) {
+                    const Sight see = sight(kr, i + 4 * hh, k1, row_pos, pre ? 0 : a.window, a.sinks);
 #pragma unroll
                     for (int k = 0; k < KB; ++k)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int key = i + k * 32 + 8 * (e >> 2) + 4 * hh + (e & 3), p = kr.pos(key);
-                            const bool see = key < k1 && p <= row_pos && (pre || a.window == 0 || p > row_pos - a.window || p < a.sinks);
-                            s[k][e] = see ? s[k][e] : NEG_INF;
-                        }
+                        for (int e = 0; e < 16; ++e) s[k][e] = see(k * 32 + 8 * (e >> 2) + (e & 3)) ? s[k][e] : NEG_INF;
                 }
-                float top = NEG_INF;
+                if (__any(m == NEG_INF)) {
+                    float top = NEG_INF;
 #pragma unroll
-                for (int k = 0; k < KB; ++k)
+                    for (int k = 0; k < KB; ++k)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
-                top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
-                // The maximum moves only when it is passed by a factor of 2^8: weights stay below 2^8, where fp32 and bf16 lose nothing.
-                if (__any(top > m + 8.0f)) {
-                    const float mn = fmaxf(m, top);
-                    const float f = mn == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-                    m = mn;
-                    l *= f;
+                        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
+                    top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
+                    if (__any(top > m + 8.0f)) {
+                        const float mn = top > m + 8.0f ? top : m;
+                        const float f = mn == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+                        m = mn;
+                        l *= f;
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d] *= f;
+                        for (int d = 0; d < DB; ++d) o[d] *= f;
+                    }
                 }
                 const float base = m == NEG_INF ? 0.0f : m;
                 // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and
@@ -261,46 +241,40 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                     }
                 });
                 __builtin_amdgcn_sched_barrier(0);
+                if (__any(l > 0x1p60f)) {
+                    const float f = fmaxf(l, __shfl_xor(l, 32)) > 0x1p60f ? 0x1p-60f : 1.0f;
+                    if (f != 1.0f) m += 60.0f;
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d] *= f;
+                }
             }
             if (i + KT < k1) {
-                shape();
-                put(buf ^ 1);
+                    put(buf ^ 1);
                 if (i + 2 * KT < k1) fetch(i + 2 * KT);
             }
             tile_barrier();
         }
-    };
-    walk(std::true_type{}, PASS_PLAIN);
-    bool fine = true;
+    l += __shfl_xor(l, 32);
+    bool fine = l < INFINITY;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) fine = fine && fabsf(o[d][e]) < INFINITY;
-    if (__syncthreads_or(!fine)) {
-        for (int pass = PASS_UP; pass <= PASS_REST; ++pass) {
-            walk(std::false_type{}, pass);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                if (pass == PASS_UP) up[d] = 0;
-                if (pass == PASS_DOWN) down[d] = 0;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    if (pass == PASS_UP) up[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
-                    else if (pass == PASS_DOWN) down[d] |= (o[d][e] > 0.0f ? 1u : 0u) << e;
-                    else {
-                        if (up[d] >> e & 1) o[d][e] += INFINITY;
-                        if (down[d] >> e & 1) o[d][e] -= INFINITY;
-                    }
-                }
-            }
-        }
+    const bool nothing = kr.n == 0 || row_pos < 0;
+    const unsigned long long odd = __ballot(!fine && !(l != l) && !nothing && r < rows);
+    const unsigned int again = (unsigned int)odd | (unsigned int)(odd >> 32);      // a bit for every row of the wave
+    for (unsigned int left = again; left; left &= left - 1) {
+        const int t = __builtin_ctz(left);
+        const RowAt at = row_at(a, pre, b, h, r0 + wave * 32 + t);
+        attn_store_again<2>(a, attn_row_again<2>(a, kr, kv, kp, vp, a.q + at.q, __shfl(row_pos, t), k0, k1), at, split);
     }
-    l += __shfl_xor(l, 32);
-    if (r >= rows) return;
+    if (r >= rows || (again >> n32 & 1)) return;
+    const RowAt to_row = row_at(a, pre, b, h, r);
 
     const int all_splits = a.splits + a.pre_splits;
     if (all_splits > 1) {
-        const int64_t part = at.lse * all_splits + split;
+        const int64_t part = to_row.lse * all_splits + split;
         if (hh == 0) a.part_ml[part] = make_float2(m, l);
         if (k0 == k1) return;
         float *to = a.part_o + part * Dd;
@@ -313,8 +287,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             }
         return;
     }
-    const bool nothing = kr.n == 0 || row_pos < 0;
-    if (a.lse && hh == 0) a.lse[at.lse] = nothing ? NEG_INF : (m == NEG_INF ? NEG_INF : m * 0.69314718055994531f) + logf(l);
+    if (a.lse && hh == 0) a.lse[to_row.lse] = nothing ? NEG_INF : (m == NEG_INF ? NEG_INF : m * 0.69314718055994531f) + logf(l);
     const float inv = 1.0f / l;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -323,7 +296,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             const int dim = 32 * d + 2 * e + 4 * hh;
             if (!FULL && dim >= Dd) continue;
             const uint2 v = make_uint2(pack_bf16(o[d][e] * inv, o[d][e + 1] * inv), pack_bf16(o[d][e + 2] * inv, o[d][e + 3] * inv));
-            *reinterpret_cast<uint2 *>(a.out + at.o + dim * 2) = nothing ? make_uint2(0, 0) : v;
+            *reinterpret_cast<uint2 *>(a.out + to_row.o + dim * 2) = nothing ? make_uint2(0, 0) : v;
         }
 }
 
