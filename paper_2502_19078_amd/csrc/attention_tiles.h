@@ -106,16 +106,19 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
         // A whole tile of consecutive cache rows has one base for all lanes (offsets in 32 bits: no row further than 32 MiB from the next)
         const int64_t row0 = kr.row(kr.pos(i), kv);
         if (i + KT <= k1 && kv.sn < (1 << 25) && kr.row(kr.pos(i + KT - 1), kv) - row0 == KT - 1) {
-            const char *kt = kp + row0 * kv.sn, *vt = vp + row0 * kv.sn;
+            const __amdgpu_buffer_rsrc_t kt = __builtin_amdgcn_make_buffer_rsrc((void *)(kp + row0 * kv.sn), 0, -1, 0x00027000);
+            const __amdgpu_buffer_rsrc_t vt = __builtin_amdgcn_make_buffer_rsrc((void *)(vp + row0 * kv.sn), 0, -1, 0x00027000);
 #pragma unroll
             for (int j = 0; j < ROWS; ++j) {
-                sk[j] = *reinterpret_cast<const u32x4 *>(kt + (lane_off + j * step_off));
-                sv[j] = *reinterpret_cast<const u32x4 *>(vt + (lane_off + j * step_off));
+                sk[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kt, lane_off, j * step_off, 0));
+                sv[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, lane_off, j * step_off, 0));
             }
         } else {
+            int key0 = i + first_key;
+            asm volatile("" : "+v"(key0));                   // (nothing of this is kept in registers across the loop)
 #pragma unroll
             for (int j = 0; j < ROWS; ++j) {
-                const int key = i + first_key + j * (256 / CPR);
+                const int key = key0 + j * (256 / CPR);
                 const int64_t off = kr.row(kr.pos(min(key, k1 - 1)), kv) * kv.sn + (in ? col : 0);
                 sk[j] = *reinterpret_cast<const u32x4 *>(kp + off);
                 sv[j] = *reinterpret_cast<const u32x4 *>(vp + off);
@@ -142,119 +145,132 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     // scaled down where a sum passes 2^60: no maxima in the loop.  Where scores rise by more than 60 powers of two within a tile, the row's
     // sums overflow and it is computed again below.
     f32x16 o[DB];
-    float m, l;
-        m = row_pos < 0 || r >= rows ? 0.0f : NEG_INF;       // (a row that sees nothing does not wait for its first key)
-        l = 0.0f;
+    float m = row_pos < 0 || r >= rows ? 0.0f : NEG_INF;     // (a row that sees nothing does not wait for its first key)
+    float l = 0.0f;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
-        if (k0 < k1) {
-            fetch(k0);
-            put(0);
-            if (k0 + KT < k1) fetch(k0 + KT);
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+    bool steady = false;                                     // every row has its maximum, and no sum has passed 2^60
+    // One tile for this wave's rows.  EDGE: some of them do not see all of it, or a maximum has to be set or moved.
+    auto multiply = [&](auto edge, int i, const char *kb, bool all) {
+        constexpr bool EDGE = decltype(edge)::value;
+        const char *vb = kb + KT * KP;
+        f32x16 s[KB];
+        const f32x16 zero = {};
+#pragma unroll
+        for (int c = 0; c < KD; ++c)
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
+                s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
+            }
+        // six fragments ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int x = 0; x < KD * KB - 6; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (EDGE) {
+            if (!all) {
+                const Sight see = sight(kr, i + 4 * hh, k1, row_pos, pre ? 0 : a.window, a.sinks);
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[k][e] = see(k * 32 + 8 * (e >> 2) + (e & 3)) ? s[k][e] : NEG_INF;
+            }
+            float top = NEG_INF;
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
+            const float grown = fmaxf(l, __shfl_xor(l, 32)), mn = top > m + 8.0f ? top : grown > 0x1p60f ? m + 60.0f : m;
+            if (__any(mn != m)) {
+                const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] *= f;
+            }
+        }
+        const float base = EDGE && m == NEG_INF ? 0.0f : m;
+        // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and the
+        // reads of V four products ahead.
+        constexpr int STEPS = 2 * KB, AHEAD = 4;
+        u32x4 vt[AHEAD], pk[2];
+        auto weight = [&](auto step, int e) {                // the e-th of the step's eight weights of this lane
+            constexpr int st = decltype(step)::value, k = st / 2, c = st % 2;
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[k][8 * c + e], scale2, -base));
+            l += p;
+            s[k][8 * c + e] = p;
+            if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
+        };
+        const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
+        auto read_v = [&](int x) {
+            const char *from = src + x / DB * 16 * VP + x % DB * 64;
+            const uint2 u0 = read_tr16(from), u1 = read_tr16(from + 8 * VP);
+            vt[x % AHEAD] = u32x4{u0.x, u0.y, u1.x, u1.y};
+        };
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) read_v(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) weight(std::integral_constant<int, 0>{}, e);
+        unrolled<STEPS>([&](auto step) {
+            constexpr int st = decltype(step)::value;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int x = st * DB + d;
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, pk[st & 1]), o[d], 0, 0, 0);
+                if (x + AHEAD < STEPS * DB) read_v(x + AHEAD);
+                if constexpr (st + 1 < STEPS) {
+#pragma unroll
+                    for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) weight(std::integral_constant<int, st + 1>{}, e);
+                }
+            }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        steady = !__any(l > 0x1p60f || (EDGE && m == NEG_INF));
+    };
+
+    if (k0 < k1) {
+        fetch(k0);
+        put(0);
+        if (k0 + KT < k1) fetch(k0 + KT);
+    }
+    tile_barrier();
+    int buf = 0, i = k0;
+    bool none = false, all = false;
+    auto look = [&]() {                                      // how the tile at i lies for this wave's rows
+        const int last = min(i + KT, k1) - 1, p_first = kr.pos(i), p_last = kr.pos(last);
+        // (a tile that begins among the sinks is looked at key by key)
+        none = idle || p_first > wave_b || (a.window && p_first >= a.sinks && p_last <= wave_a - a.window && wave_a >= 0);
+        all = last == i + KT - 1 && !ragged && (pre || (p_last <= wave_a && (a.window == 0 || p_first > wave_b - a.window || p_last < a.sinks)));
+    };
+    auto next = [&]() {                                      // the next tile into LDS, the one after it on its way
+        if (i + KT < k1) {
+            put(buf ^ 1);
+            if (i + 2 * KT < k1) fetch(i + 2 * KT);
         }
         tile_barrier();
-        int buf = 0;
-        for (int i = k0; i < k1; i += KT, buf ^= 1) {
-            const int last = min(i + KT, k1) - 1, p_first = kr.pos(i), p_last = kr.pos(last);
-            // (a tile that begins among the sinks is looked at key by key)
-            const bool none = idle || p_first > wave_b || (a.window && p_first >= a.sinks && p_last <= wave_a - a.window && wave_a >= 0);
-            const bool all = last == i + KT - 1 && !ragged && (pre || (p_last <= wave_a && (a.window == 0 || p_first > wave_b - a.window || p_last < a.sinks)));
-            if (!none) {
-                const char *kb = lds + buf * BUF, *vb = kb + KT * KP;
-                f32x16 s[KB];
-                const f32x16 zero = {};
-#pragma unroll
-                for (int c = 0; c < KD; ++c)
-#pragma unroll
-                    for (int k = 0; k < KB; ++k) {
-                        const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
-                        s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
-                    }
-                // six fragments ahead of the products
-                __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-                for (int x = 0; x < KD * KB - 6; ++x) {
-                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                }
-                __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                if (!all) {
-                    const Sight see = sight(kr, i + 4 * hh, k1, row_pos, pre ? 0 : a.window, a.sinks);
-#pragma unroll
-                    for (int k = 0; k < KB; ++k)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[k][e] = see(k * 32 + 8 * (e >> 2) + (e & 3)) ? s[k][e] : NEG_INF;
-                }
-                if (__any(m == NEG_INF)) {
-                    float top = NEG_INF;
-#pragma unroll
-                    for (int k = 0; k < KB; ++k)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
-                    top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
-                    if (__any(top > m + 8.0f)) {
-                        const float mn = top > m + 8.0f ? top : m;
-                        const float f = mn == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-                        m = mn;
-                        l *= f;
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) o[d] *= f;
-                    }
-                }
-                const float base = m == NEG_INF ? 0.0f : m;
-                // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and
-                // the reads of V four products ahead.
-                constexpr int STEPS = 2 * KB, AHEAD = 4;
-                u32x4 vt[AHEAD], pk[2];
-                auto weight = [&](auto step, int e) {        // the e-th of the step's eight weights of this lane
-                    constexpr int st = decltype(step)::value, k = st / 2, c = st % 2;
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[k][8 * c + e], scale2, -base));
-                    l += p;
-                    s[k][8 * c + e] = p;
-                    if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
-                };
-                const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
-                auto read_v = [&](int x) {
-                    const char *from = src + x / DB * 16 * VP + x % DB * 64;
-                    const uint2 u0 = read_tr16(from), u1 = read_tr16(from + 8 * VP);
-                    vt[x % AHEAD] = u32x4{u0.x, u0.y, u1.x, u1.y};
-                };
-#pragma unroll
-                for (int x = 0; x < AHEAD; ++x) read_v(x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) weight(std::integral_constant<int, 0>{}, e);
-                unrolled<STEPS>([&](auto step) {
-                    constexpr int st = decltype(step)::value;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        const int x = st * DB + d;
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, pk[st & 1]), o[d], 0, 0, 0);
-                        if (x + AHEAD < STEPS * DB) read_v(x + AHEAD);
-                        if constexpr (st + 1 < STEPS) {
-#pragma unroll
-                            for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) weight(std::integral_constant<int, st + 1>{}, e);
-                        }
-                    }
-                });
-                __builtin_amdgcn_sched_barrier(0);
-                if (__any(l > 0x1p60f)) {
-                    const float f = fmaxf(l, __shfl_xor(l, 32)) > 0x1p60f ? 0x1p-60f : 1.0f;
-                    if (f != 1.0f) m += 60.0f;
-                    l *= f;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d] *= f;
-                }
-            }
-            if (i + KT < k1) {
-                    put(buf ^ 1);
-                if (i + 2 * KT < k1) fetch(i + 2 * KT);
-            }
-            tile_barrier();
+        buf ^= 1;
+        i += KT;
+    };
+    // The waves of a workgroup may be in different loops; every tile is one barrier in both.
+    while (i < k1) {
+        look();
+        if (!none) multiply(std::true_type{}, i, lds + buf * BUF, all);
+        next();
+        for (; i < k1; next()) {
+            look();
+            if (none || !all || !steady) break;
+            multiply(std::false_type{}, i, lds + buf * BUF, true);
         }
+    }
     l += __shfl_xor(l, 32);
     bool fine = l < INFINITY;
 #pragma unroll
