@@ -548,30 +548,30 @@ def attn_workspace_bytes(B: int, T: int, Hq: int, d: int) -> int:
 class KVCache:
     """Keys and values [batch][heads][capacity][d] on the GPU: two tensors (views with any strides, d contiguous) of one shape and one
     set of strides.  ring = 0: row n holds position n.  ring > 0: positions from n_sink on share `ring` rows behind the first n_sink."""
-    __slots__ = ("k", "v", "n_sink", "ring", "_c", "_ref")
+    __slots__ = ("k", "v", "n_sink", "ring", "heads", "d", "dtype", "device_index", "_c", "_ref")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, n_sink: int = 0, ring: int = 0):
-        shape, stride = k.shape, k.stride()
-        assert k.is_cuda and v.is_cuda and len(shape) == 4 and v.shape == shape and v.dtype == k.dtype and v.device == k.device
+        shape, stride, dtype = k.shape, k.stride(), k.dtype
+        assert k.is_cuda and len(shape) == 4 and v.shape == shape and v.dtype is dtype and v.get_device() == k.get_device()
         assert stride[3] == 1 and v.stride() == stride, "k and v need one set of strides, the values of a head contiguous"
         B, H, N, D = shape
         self.k, self.v, self.n_sink, self.ring = k, v, n_sink, ring
+        self.heads, self.d, self.dtype, self.device_index = H, D, dtype, k.get_device()
         self._c = _CKvCache(k.data_ptr(), v.data_ptr(), stride[0] if B > 1 else 0, stride[1] if H > 1 else 0, stride[2] if N > 1 else 0,
                             B, H, D, N, _dtype_code(k), n_sink, ring)
         self._ref = C.byref(self._c)
 
 
-def _heads(x: torch.Tensor, cache: KVCache, what: str):
-    """clada_heads of x [B][T][H][d]."""
-    B, T, H, D = x.shape
-    st = x.stride()
-    assert x.is_cuda and x.dtype == cache.k.dtype and x.device == cache.k.device and D == cache._c.d and st[3] == 1, \
+def _heads(x: torch.Tensor, shape, cache: KVCache, what: str):
+    """clada_heads of x [B][T][H][d], whose shape is `shape`.  (A dimension of one row has no stride to speak of.)"""
+    sb, st, sh, sd = x.stride()
+    assert x.get_device() == cache.device_index and x.dtype is cache.dtype and sd == 1 and shape[3] == cache.d, \
         f"{what}: type, device, head size or strides do not fit the cache"
-    return C.byref(_CHeads(x.data_ptr(), st[0] if B > 1 else 0, st[1] if T > 1 else 0, st[2] if H > 1 else 0))
+    return C.byref(_CHeads(x.data_ptr(), sb if shape[0] > 1 else 0, st if shape[1] > 1 else 0, sh if shape[2] > 1 else 0))
 
 
 def _ints(x: torch.Tensor, n: int, cache: KVCache, what: str):
-    assert x.is_cuda and x.dtype == torch.int32 and x.is_contiguous() and x.numel() == n and x.device == cache.k.device, \
+    assert x.dtype is torch.int32 and x.numel() == n and x.is_contiguous() and x.get_device() == cache.device_index, \
         f"{what}: expected {n} contiguous int32 on the cache's device"
     return x.data_ptr()
 
@@ -601,25 +601,24 @@ def qk_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tenso
     """Norm for each head (norm None: where a weight is given; True without weights: the bare norm), rotation, and keys and values into the cache.  q [B][T][Hq][d], k and v
     [B][T][heads][d] (any strides, d contiguous), positions [B][T] int32 -> rotated queries (None without q)."""
     x = q if q is not None else k
-    B, T = x.shape[0], x.shape[1]
-    cq = co = ck = cv = None
-    Hq = 0
+    shape = x.shape
+    B, T, Hq, _ = shape
+    cq = co = ck = cv = c_norm = None
     if q is not None:
-        Hq = q.shape[2]
-        assert q.shape[0] == B and q.shape[1] == T
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        assert out.shape == q.shape
-        cq, co = _heads(q, cache, "q"), _heads(out, cache, "out")
+            out = torch.empty_like(q)
+        else:
+            assert out.shape == shape
+        cq, co = _heads(q, shape, cache, "q"), _heads(out, shape, cache, "out")
     if k is not None:
-        assert v is not None and k.shape == v.shape and k.shape[0] == B and k.shape[1] == T and k.shape[2] == cache._c.heads
-        ck, cv = _heads(k, cache, "k"), _heads(v, cache, "v")
+        kshape = k.shape
+        assert v is not None and v.shape == kshape and kshape[0] == B and kshape[1] == T and kshape[2] == cache.heads
+        ck, cv = _heads(k, kshape, cache, "k"), _heads(v, kshape, cache, "v")
     turns = plan.turns
-    assert turns.is_cuda and turns.dtype == torch.int64 and turns.is_contiguous()
-    c_norm = None
+    assert turns.get_device() == cache.device_index and turns.dtype is torch.int64 and turns.is_contiguous()
     if norm or (norm is None and (q_norm is not None or k_norm is not None)):
         for w in (q_norm, k_norm):
-            assert w is None or (w.is_cuda and w.dtype == x.dtype and w.is_contiguous() and w.numel() == cache._c.d)
+            assert w is None or (w.get_device() == cache.device_index and w.dtype is cache.dtype and w.is_contiguous() and w.numel() == cache.d)
         c_norm = C.byref(_CHeadNorm(_ptr(q_norm), _ptr(k_norm), eps, norm_offset))
     ctx.check(ctx._lib.clada_qk_rope(ctx._h, C.byref(_CRope(turns.data_ptr(), 2 * turns.numel(), plan.layout, plan.magnitude)), c_norm, B, T, Hq, cq,
                                      ck, cv, _ints(positions, B * T, cache, "positions"),
@@ -631,14 +630,16 @@ def window_attn(ctx: Context, q: torch.Tensor, cache: KVCache, lens: torch.Tenso
                 sinks: int = 0, scale: float | None = None, out: torch.Tensor | None = None, want_lse: bool = False):
     """Causal attention of q [B][T][Hq][d] over the cache; lens [B] int32 tokens held (the call's own among them), q_lens [B] int32
     queries of every sequence (None: T).  window 0: everything is visible.  scale None: d^-0.5.  Returns out, or (out, lse [B][T][Hq])."""
-    B, T, Hq, D = q.shape
+    shape = q.shape
+    B, T, Hq, D = shape
     if out is None:
-        out = torch.empty(B, T, Hq, D, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape
-    lse = torch.empty(B, T, Hq, dtype=torch.float32, device=q.device) if want_lse else None
-    ctx.check(ctx._lib.clada_window_attn(ctx._h, _heads(q, cache, "q"), cache._ref, _ints(lens, B, cache, "lens"),
+        out = torch.empty_like(q)
+    else:
+        assert out.shape == shape
+    lse = torch.empty((B, T, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    ctx.check(ctx._lib.clada_window_attn(ctx._h, _heads(q, shape, cache, "q"), cache._ref, _ints(lens, B, cache, "lens"),
                                          None if q_lens is None else _ints(q_lens, B, cache, "q_lens"), B, T, Hq, window, sinks,
-                                         D ** -0.5 if scale is None else scale, _heads(out, cache, "out"), _ptr(lse), _stream(q)))
+                                         D ** -0.5 if scale is None else scale, _heads(out, shape, cache, "out"), _ptr(lse), _stream(q)))
     return (out, lse) if want_lse else out
 
 
@@ -648,12 +649,15 @@ def shared_prefix_attn(ctx: Context, q: torch.Tensor, prefix: KVCache, prefix_le
     sequence's own in `cache`.  Returns out, or (out, lse [B][Hq])."""
     B, Hq, D = q.shape
     if out is None:
-        out = torch.empty(B, Hq, D, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and prefix.k.device == cache.k.device
-    lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if want_lse else None
-    ctx.check(ctx._lib.clada_shared_prefix_attn(ctx._h, _heads(q.unsqueeze(1), cache, "q"), prefix._ref, prefix_len, cache._ref,
+        out = torch.empty_like(q)
+    else:
+        assert out.shape == q.shape
+    assert prefix.device_index == cache.device_index
+    lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    shape = (B, 1, Hq, D)
+    ctx.check(ctx._lib.clada_shared_prefix_attn(ctx._h, _heads(q.unsqueeze(1), shape, cache, "q"), prefix._ref, prefix_len, cache._ref,
                                                 _ints(lens, B, cache, "lens"), B, Hq, D ** -0.5 if scale is None else scale,
-                                                _heads(out.unsqueeze(1), cache, "out"), _ptr(lse), _stream(q)))
+                                                _heads(out.unsqueeze(1), shape, cache, "out"), _ptr(lse), _stream(q)))
     return (out, lse) if want_lse else out
 
 

@@ -51,9 +51,9 @@ __device__ __forceinline__ unsigned int pack_bf16(float lo, float hi)      // ro
 
 // Where a row's query and output lie.
 struct RowAt { int64_t q, o, lse; };
-__device__ __forceinline__ RowAt row_at(const AttnArgs &a, bool pre, int b, int h, int r)
+__device__ __forceinline__ RowAt row_at(const AttnArgs &a, bool pre, int b, int h, int r, int i)      // i = r / G
 {
-    const int i = r / a.G, hq = h * a.G + (r - i * a.G);
+    const int hq = h * a.G + (r - i * a.G);
     const int bb = pre ? i : b, t = pre ? 0 : i;
     return {bb * a.q_sb + t * a.q_st + hq * a.q_sh, bb * a.o_sb + t * a.o_st + hq * a.o_sh, ((int64_t)bb * a.T + t) * a.Hq + hq};
 }
@@ -112,11 +112,11 @@ __device__ __forceinline__ Sight sight(const KeyRange &kr, int base, int end, in
 }
 
 // Tokens that a sequence holds and queries that the call brings for it, whatever the arrays say.
-__device__ __forceinline__ void sequence_lens(const AttnArgs &a, int b, int &len, int &qlen)
+__device__ __forceinline__ void sequence_lens(const AttnArgs &a, int len_b, int qlen_b, int &len, int &qlen)
 {
-    len = max(a.lens[b], 0);
+    len = max(len_b, 0);
     if (a.kv.ring == 0) len = min(len, a.kv.capacity);
-    qlen = a.q_lens ? min(max(a.q_lens[b], 0), a.T) : a.T;
+    qlen = min(max(qlen_b, 0), a.T);
 }
 
 // A product over a tile gives every row every key of it, and a weight of zero (or the lower half of a weight) times a value that is not finite

@@ -36,46 +36,55 @@ k_attn_prefix(const AttnArgs a)
     else attn_rows<2, DP, 1, FULL>(a, false, id - pre_blocks, lds);
 }
 
-// One workgroup a row: its splits' partial results joined in order of the split.  TPR threads hold 4 values each of a row; the 256 / TPR
-// groups take splits in turn and are joined through LDS.
+// One workgroup a row: its splits' partial results joined in a fixed order.  TPR threads hold 4 values each of a row; the 256 / TPR groups take
+// splits in turn and are joined through LDS.  A split's factor is computed by one thread for all.
 template <int ES, int TPR>
 __global__ void __launch_bounds__(256)
 k_attn_join(const AttnArgs a)
 {
     constexpr int GR = 256 / TPR;
-    __shared__ float s_l[GR];
+    __shared__ float s_f[256], s_red[8];
     __shared__ f32x4 s_o[GR][TPR];
     const int64_t row = blockIdx.x;
-    const int splits = a.splits + a.pre_splits;
-    const int gr = threadIdx.x / TPR, dim = threadIdx.x % TPR * 4;
-    const float2 *ml = a.part_ml + row * splits;
-    float top = NEG_INF;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, ml[s].x);
-    float l = 0.0f;
+    const int splits = a.splits + a.pre_splits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int gr = tid / TPR, dim = tid % TPR * 4;
+    float l = 0.0f, top = NEG_INF;
     f32x4 o = {0, 0, 0, 0};
-    for (int s = gr; s < splits; s += GR) {
-        const float2 v = ml[s];
-        if (v.x == NEG_INF && v.y == 0.0f) continue;         // a split without keys has written no values
-        const float f = v.x == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(v.x - top);
-        l += v.y * f;
-        if (dim < a.D) o += *reinterpret_cast<const f32x4 *>(a.part_o + (row * splits + s) * a.D + dim) * f;
+    for (int s0 = 0; s0 < splits; s0 += 256) {               // (512 splits at most: two rounds)
+        const float2 v = s0 + tid < splits ? a.part_ml[row * splits + s0 + tid] : make_float2(NEG_INF, 0.0f);
+        const float most = wave_max(v.x);
+        __syncthreads();
+        if (lane == 0) s_red[wave] = most;
+        __syncthreads();
+        const float mn = fmaxf(top, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
+        // a split without keys has written no values: none are read for it
+        const float f = v.x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(v.x - mn), g = top == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(top - mn);
+        s_f[tid] = v.y == 0.0f ? -1.0f : f;
+        const float sum = wave_sum(v.x == NEG_INF ? v.y : v.y * f);
+        if (lane == 0) s_red[4 + wave] = sum;
+        __syncthreads();
+        l = l * g + ((s_red[4] + s_red[5]) + (s_red[6] + s_red[7]));
+        o *= g;
+        top = mn;
+        const int n = min(splits - s0, 256);
+#pragma unroll 4
+        for (int s = gr; s < n; s += GR) {
+            const float fs = s_f[s];
+            if (fs != -1.0f && dim < a.D) o += *reinterpret_cast<const f32x4 *>(a.part_o + (row * splits + s0 + s) * a.D + dim) * fs;
+        }
     }
-    s_o[gr][threadIdx.x % TPR] = o;
-    if (threadIdx.x % TPR == 0) s_l[gr] = l;
+    s_o[gr][tid % TPR] = o;
     __syncthreads();
     if (gr) return;
 #pragma unroll
-    for (int k = 1; k < GR; ++k) {
-        l += s_l[k];
-        o += s_o[k][threadIdx.x];
-    }
+    for (int k = 1; k < GR; ++k) o += s_o[k][tid];
     const int hq = (int)(row % a.Hq);
     const int64_t bt = row / a.Hq;
-    const int b = (int)(bt / a.T), t = (int)(bt % a.T);
+    const int b = a.T == 1 ? (int)bt : (int)(bt / a.T), t = (int)(bt - (int64_t)b * a.T);
     int len, qlen;
-    sequence_lens(a, b, len, qlen);
+    sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
     const bool none = a.pre_splits ? a.pre_n + len == 0 : t >= qlen || len - qlen + t < 0;
-    if (a.lse && threadIdx.x == 0) a.lse[row] = none ? NEG_INF : top * 0.69314718055994531f + logf(l);
+    if (a.lse && tid == 0) a.lse[row] = none ? NEG_INF : top * 0.69314718055994531f + logf(l);
     if (dim >= a.D) return;
     o = none ? f32x4{0, 0, 0, 0} : o * (1.0f / l);
     char *to = a.out + b * a.o_sb + t * a.o_st + hq * a.o_sh;

@@ -21,7 +21,7 @@ template <int ES, int DP, int NT>
 struct RowsShape {
     static constexpr int KB = ES == 2 ? 2 : 1, KS = 16 * KB; // keys of a step
     static constexpr int PITCH = DP * 2 + 32;                // V in LDS: rows 8 banks apart modulo 64
-    static constexpr int V_LDS = ES == 2 ? 4 * 32 * PITCH : 0, J_LDS = 2 * NT * 16 * (DP * 4 + 8);
+    static constexpr int V_LDS = ES == 2 ? 4 * 32 * PITCH : 0, J_LDS = DP * 256 + 512 * NT + 16;     // of the join: outputs and maxima of four waves
     static constexpr int LDS = V_LDS > J_LDS ? V_LDS : J_LDS;
 };
 
@@ -61,6 +61,25 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
     const int all_splits = a.splits + a.pre_splits, part = pre ? split : a.pre_splits + split;
     const int r0 = tile * 16 * NT;
     const AttnKV &kv = pre ? a.pre : a.kv;
+
+    // this lane's rows: queries as the second operand.  (Loaded ahead of the lengths, which the keys wait for.)
+    const int len_b = pre ? 0 : a.lens[b], qlen_b = pre || !a.q_lens ? a.T : a.q_lens[b];
+    u32x4 qf[NT][CH];
+    int row_pos[NT];
+    RowAt at[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = min(r0 + nt * 16 + n16, rows - 1);
+        row_pos[nt] = !pre && a.T == 1 ? 0 : r / a.G;        // (the row's token for now)
+        at[nt] = row_at(a, pre, b, h, r, row_pos[nt]);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int off = 64 * c + 16 * g;
+            const bool in = FULL || off < Dd * ES;
+            qf[nt][c] = *reinterpret_cast<const u32x4 *>(a.q + at[nt].q + (in ? off : 0));
+            if (!in) qf[nt][c] = u32x4{0, 0, 0, 0};
+        }
+    }
     KeyRange kr;
     int first_pos = 0, qlen = a.T;
     if (pre) {
@@ -69,35 +88,21 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
         kr.pos_a = kr.pos_b = a.pre_n;
     } else {
         int len;
-        sequence_lens(a, b, len, qlen);
+        sequence_lens(a, len_b, qlen_b, len, qlen);
         first_pos = len - qlen;
-        if (a.pre_splits) {                                  // behind a prefix: all of the sequence's rows
+        if (a.pre_splits)                                    // behind a prefix: all of the sequence's rows
             kr = key_range(kv, len - 1, 0, 0, 0, 0);
-        } else
+        else if (a.T == 1)
+            kr = key_range(kv, first_pos, 0, qlen - 1, a.window, a.sinks);
+        else
             kr = key_range(kv, first_pos, r0 / a.G, min(min(r0 + 16 * NT - 1, rows - 1) / a.G, qlen - 1), a.window, a.sinks);
     }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) row_pos[nt] = pre || a.pre_splits ? 0 : row_pos[nt] < qlen ? first_pos + row_pos[nt] : -1;
     const bool one_pos = pre || a.pre_splits || kr.pos_a == kr.pos_b;      // all rows see the same keys
     int chunk = (kr.n + splits - 1) / splits;
     chunk = (chunk + 31) & ~31;
     const int k0 = min(split * chunk, kr.n), k1 = min(k0 + chunk, kr.n);
-
-    // this lane's rows: queries as the second operand, and the positions that they may see
-    u32x4 qf[NT][CH];
-    int row_pos[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = r0 + nt * 16 + n16;
-        const RowAt at = row_at(a, pre, b, h, min(r, rows - 1));
-        const int i = min(r, rows - 1) / a.G;
-        row_pos[nt] = pre || a.pre_splits ? 0 : i < qlen ? first_pos + i : -1;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int off = 64 * c + 16 * g;
-            const bool in = FULL || off < Dd * ES;
-            qf[nt][c] = *reinterpret_cast<const u32x4 *>(a.q + at.q + (in ? off : 0));
-            if (!in) qf[nt][c] = u32x4{0, 0, 0, 0};
-        }
-    }
 
     const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
     char *my_v = lds + wave * 32 * PITCH;
@@ -253,57 +258,52 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
         }
     }
 
-    // join the waves: 2 and 3 hand over to 0 and 1, then 1 to 0
+    // The waves' results side by side in LDS; then every wave joins a part of each row's outputs: v[nt][x] are the four from dim(x) on.
+    constexpr int OUT = (DB + 3) / 4;
+    auto dim = [&](int x) { return ES == 2 ? 16 * (wave + 4 * x) + 4 * g : 64 * x + 16 * g + 4 * wave; };
+    float2 *s_ml = reinterpret_cast<float2 *>(lds + DP * 256);
+    unsigned int *s_again = reinterpret_cast<unsigned int *>(lds + DP * 256 + 512 * NT);
+    f32x4 v[NT][OUT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         l[nt] += __shfl_xor(l[nt], 16);
         l[nt] += __shfl_xor(l[nt], 32);
-    }
-#pragma unroll
-    for (int step = 2; step >= 1; step >>= 1) {
         __syncthreads();
-        if (wave >= step && wave < 2 * step) {
-            char *to = lds + (wave - step) * NT * 16 * (DP * 4 + 8);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+        for (int d = 0; d < DB; ++d) reinterpret_cast<f32x4 *>(lds)[(wave * DB + d) * 64 + lane] = o[nt][d];
+        if (g == 0) s_ml[(wave * NT + nt) * 16 + n16] = make_float2(m[nt], l[nt]);
+        if (nt == 0 && threadIdx.x == 0) *s_again = 0;
+        __syncthreads();
+        float2 ml[4];
 #pragma unroll
-                for (int d = 0; d < DB; ++d) reinterpret_cast<f32x4 *>(to)[(nt * DB + d) * 64 + lane] = o[nt][d];
-                if (g == 0) reinterpret_cast<float2 *>(to + NT * 16 * DP * 4)[nt * 16 + n16] = make_float2(m[nt], l[nt]);
+        for (int w = 0; w < 4; ++w) ml[w] = s_ml[(w * NT + nt) * 16 + n16];
+        m[nt] = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+        l[nt] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < OUT; ++x) v[nt][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = ml[w].x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(ml[w].x - m[nt]);
+            l[nt] += ml[w].y * f;
+#pragma unroll
+            for (int x = 0; x < OUT; ++x) {
+                if (ES == 2) {
+                    if (DB % 4 == 0 || wave + 4 * x < DB) v[nt][x] += reinterpret_cast<const f32x4 *>(lds)[(w * DB + wave + 4 * x) * 64 + lane] * f;
+                } else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[nt][x][e] += reinterpret_cast<const float *>(lds)[((w * DB + 4 * x + e) * 64 + lane) * 4 + wave] * f;
             }
         }
-        __syncthreads();
-        if (wave < step) {
-            const char *from = lds + wave * NT * 16 * (DP * 4 + 8);
+        bool fine = l[nt] < INFINITY;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float2 ml = reinterpret_cast<const float2 *>(from + NT * 16 * DP * 4)[nt * 16 + n16];
-                const float mn = fmaxf(m[nt], ml.x);
-                const float f0 = m[nt] == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(m[nt] - mn);
-                const float f1 = ml.x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mn);
+        for (int x = 0; x < OUT; ++x)
 #pragma unroll
-                for (int d = 0; d < DB; ++d) o[nt][d] = o[nt][d] * f0 + reinterpret_cast<const f32x4 *>(from)[(nt * DB + d) * 64 + lane] * f1;
-                m[nt] = mn;
-                l[nt] = l[nt] * f0 + ml.y * f1;
-            }
-        }
-    }
-    // rows that are not finite, bit for row, from wave 0 to all
-    __syncthreads();
-    unsigned int *s_again = reinterpret_cast<unsigned int *>(lds);
-    if (wave == 0) {
-        unsigned int again = 0;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            bool fine = l[nt] < INFINITY;
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) fine = fine && fabsf(o[nt][d][e]) < INFINITY;
-            unsigned long long odd = __ballot(!fine && !(l[nt] != l[nt]) && row_pos[nt] >= 0 && r0 + nt * 16 + n16 < rows);
+            for (int e = 0; e < 4; ++e) fine = fine && fabsf(v[nt][x][e]) < INFINITY;
+        unsigned long long odd = __ballot(!fine && !(l[nt] != l[nt]) && row_pos[nt] >= 0 && r0 + nt * 16 + n16 < rows);
+        if (odd) {
             odd |= odd >> 32;
-            again |= (unsigned int)((odd | odd >> 16) & 0xffff) << (nt * 16);
+            if (lane == 0) atomicOr(s_again, (unsigned int)((odd | odd >> 16) & 0xffff) << (nt * 16));
         }
-        if (lane == 0) *s_again = again;
     }
     __syncthreads();
     const unsigned int again = kr.n ? __builtin_amdgcn_readfirstlane(*s_again) : 0u;
@@ -311,43 +311,35 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
         for (int t = wave; t < 16 * NT; t += 4) {
             if (!(again >> t & 1)) continue;
             const int r = r0 + t;
-            const RowAt at = row_at(a, pre, b, h, r);
-            attn_store_again<ES>(a, attn_row_again<ES>(a, kr, kv, kp, vp, a.q + at.q, pre || a.pre_splits ? INT32_MAX : first_pos + r / a.G, k0, k1), at, part);
+            const RowAt row = row_at(a, pre, b, h, r, r / a.G);
+            attn_store_again<ES>(a, attn_row_again<ES>(a, kr, kv, kp, vp, a.q + row.q, pre || a.pre_splits ? INT32_MAX : first_pos + r / a.G, k0, k1), row, part);
         }
     }
-    if (wave) return;
 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int r = r0 + nt * 16 + n16;
-        if (r >= rows || (again >> (nt * 16 + n16) & 1)) continue;
-        const RowAt at = row_at(a, pre, b, h, r);
+        if (r0 + nt * 16 + n16 >= rows || (again >> (nt * 16 + n16) & 1)) continue;
         if (all_splits > 1) {
-            const int64_t at_part = at.lse * all_splits + part;
-            if (g == 0) a.part_ml[at_part] = make_float2(m[nt], l[nt]);
+            const int64_t at_part = at[nt].lse * all_splits + part;
+            if (g == 0 && wave == 0) a.part_ml[at_part] = make_float2(m[nt], l[nt]);
             if (k0 == k1) continue;                          // nothing to read for this split
             float *to = a.part_o + at_part * Dd;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const f32x4 v = ES == 2 ? o[nt][d] : f32x4{o[nt][d / 4 * 4][d % 4], o[nt][d / 4 * 4 + 1][d % 4], o[nt][d / 4 * 4 + 2][d % 4], o[nt][d / 4 * 4 + 3][d % 4]};
-                const int dim = ES == 2 ? 16 * d + 4 * g : 64 * (d / 4) + 16 * g + 4 * (d % 4);
-                if (FULL || dim < Dd) *reinterpret_cast<f32x4 *>(to + dim) = v;
-            }
+            for (int x = 0; x < OUT; ++x)
+                if (dim(x) < Dd) *reinterpret_cast<f32x4 *>(to + dim(x)) = v[nt][x];
             continue;
         }
         const bool none = kr.n == 0 || row_pos[nt] < 0;
-        if (a.lse && g == 0) a.lse[at.lse] = none ? NEG_INF : (m[nt] == NEG_INF ? NEG_INF : m[nt] * 0.69314718055994531f) + logf(l[nt]);
-        const float inv = none ? 0.0f : 1.0f / l[nt];
+        if (a.lse && g == 0 && wave == 0) a.lse[at[nt].lse] = none ? NEG_INF : (m[nt] == NEG_INF ? NEG_INF : m[nt] * 0.69314718055994531f) + logf(l[nt]);
+        const float inv = 1.0f / l[nt];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            f32x4 v = ES == 2 ? o[nt][d] : f32x4{o[nt][d / 4 * 4][d % 4], o[nt][d / 4 * 4 + 1][d % 4], o[nt][d / 4 * 4 + 2][d % 4], o[nt][d / 4 * 4 + 3][d % 4]};
-            const int dim = ES == 2 ? 16 * d + 4 * g : 64 * (d / 4) + 16 * g + 4 * (d % 4);
-            if (!FULL && dim >= Dd) continue;
-            v = none ? f32x4{0, 0, 0, 0} : v * inv;
+        for (int x = 0; x < OUT; ++x) {
+            if (dim(x) >= Dd) continue;
+            const f32x4 y = none ? f32x4{0, 0, 0, 0} : v[nt][x] * inv;
             if (ES == 2)
-                *reinterpret_cast<uint2 *>(a.out + at.o + dim * 2) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                *reinterpret_cast<uint2 *>(a.out + at[nt].o + dim(x) * 2) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
             else
-                *reinterpret_cast<f32x4 *>(a.out + at.o + dim * 4) = v;
+                *reinterpret_cast<f32x4 *>(a.out + at[nt].o + dim(x) * 4) = y;
         }
     }
 }

@@ -67,7 +67,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
         kr.pos_a = kr.pos_b = a.pre_n;
     } else {
         int len;
-        sequence_lens(a, b, len, qlen);
+        sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
         first_pos = len - qlen;
         kr = key_range(kv, first_pos, r0 / a.G, min(min(r0 + 127, rows - 1) / a.G, qlen - 1), a.window, a.sinks);
     }
@@ -92,7 +92,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     for (int c = 0; c < KD; ++c) {
         const int off = 32 * c + 16 * hh;
         const bool in = FULL || off < Dd * 2;
-        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + row_at(a, pre, b, h, rc).q + (in ? off : 0));
+        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + row_at(a, pre, b, h, rc, rc / a.G).q + (in ? off : 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) qf[c][e] = in ? qf[c][e] ^ flip : 0u;
     }
@@ -282,11 +282,11 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     const unsigned int again = (unsigned int)odd | (unsigned int)(odd >> 32);      // a bit for every row of the wave
     for (unsigned int left = again; left; left &= left - 1) {
         const int t = __builtin_ctz(left);
-        const RowAt at = row_at(a, pre, b, h, r0 + wave * 32 + t);
+        const RowAt at = row_at(a, pre, b, h, r0 + wave * 32 + t, (r0 + wave * 32 + t) / a.G);
         attn_store_again<2>(a, attn_row_again<2>(a, kr, kv, kp, vp, a.q + at.q, __shfl(row_pos, t), k0, k1), at, split);
     }
     if (r >= rows || (again >> n32 & 1)) return;
-    const RowAt to_row = row_at(a, pre, b, h, r);
+    const RowAt to_row = row_at(a, pre, b, h, r, r / a.G);
 
     const int all_splits = a.splits + a.pre_splits;
     if (all_splits > 1) {
