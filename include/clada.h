@@ -471,7 +471,7 @@ typedef struct {
 clada_status clada_rope_turns(clada_ctx *ctx, int32_t rotary_dim, const clada_rope_scaling *scaling, uint64_t *turns, float *magnitude);
 
 /* Norms of queries and keys for each head: x / sqrt(mean(x^2) + eps) * (weight + offset), ahead of the rotation; weights [d] in
- * the cache's dtype, NULL for no factor (offset then plays no part). */
+ * the cache's dtype, 16-byte aligned as the turns are, NULL for no factor (offset then plays no part). */
 typedef struct {
     const void *q_weight, *k_weight;
     float eps, offset;

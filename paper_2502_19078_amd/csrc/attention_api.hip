@@ -45,11 +45,11 @@ AttnKV kv_of(const clada_kv_cache *c)
     return {(const char *)c->k, (const char *)c->v, c->stride_b * es, c->stride_h * es, c->stride_n * es, c->capacity, c->n_sink, c->ring};
 }
 
-// Splits of `keys` keys for `units` tiles, so that the launch fills the chip: two workgroups a compute unit, no split under 128 keys.  Up to 1024
-// keys a workgroup is done with all of them (eight steps of its waves) by the time a second launch would have joined splits.
-int splits_for(int64_t units, int64_t keys, int num_cu, bool joined)
+// Splits of `keys` keys for `units` tiles, so that the launch fills the chip: two workgroups a compute unit, no split under 128 keys (one step of its
+// waves).  513 keys of one key head of 256 values: four splits and the launch that joins them 15 us, one workgroup 26 us (a compute unit
+// loads 26 bytes a clock).
+int splits_for(int64_t units, int64_t keys, int num_cu)
 {
-    if (keys <= 1024 && !joined) return 1;
     const int64_t want = (2 * (int64_t)num_cu + units - 1) / units, most = (keys + 127) / 128;
     int64_t s = want < most ? want : most;
     if (s > MAX_SPLITS) s = MAX_SPLITS;
@@ -148,7 +148,7 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
         const int64_t seen = (int64_t)window + sinks + tile / a.G;
         if (seen < keys) keys = seen;
     }
-    a.splits = splits_for(units, keys, ctx->num_cu, false);
+    a.splits = splits_for(units, keys, ctx->num_cu);
     if (units * a.splits > INT32_MAX) return clada_fail(ctx, CLADA_ERR_SHAPE, "the call has too many rows");
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
@@ -183,8 +183,8 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     const int tile = path == ATTN_ROWS16 ? 16 : path == ATTN_ROWS32 ? 32 : 128, own = path == ATTN_ROWS32 ? 32 : 16;
     a.pre_tiles = (B * a.G + tile - 1) / tile;
     a.own_tiles = (a.G + own - 1) / own;
-    a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu, true);
-    a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu, true);
+    a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
+    a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
     if ((st = place_parts(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
     return CLADA_OK;

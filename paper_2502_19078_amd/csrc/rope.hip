@@ -8,7 +8,7 @@
 // value's rounding.  f_i is therefore held as a 64-bit fraction of a turn, and the integer product wraps whole turns away exactly.
 #include <math.h>
 
-#include "clada_internal.h"
+#include "attention.h"
 
 namespace {
 
@@ -21,7 +21,7 @@ struct RopeArgs {
     const void *qw, *kw;
     int T, tokens, Hq, Hk, D, R;                      // Hk: key heads stored (0: queries only)
     int slabs, capacity, n_sink, ring;
-    float eps, offset, magnitude;
+    float eps, offset, magnitude, inv_d;
     int norm;
 };
 
@@ -30,18 +30,27 @@ __device__ __forceinline__ u32x4 pack_row16(const float *f)
 {
     u32x4 v;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        v[k] = ES == 2 ? (f32_to_bf16_bits(f[2 * k]) | (f32_to_bf16_bits(f[2 * k + 1]) << 16)) : __float_as_uint(f[k]);
+    for (int k = 0; k < 4; ++k) v[k] = ES == 2 ? pack_bf16(f[2 * k], f[2 * k + 1]) : __float_as_uint(f[k]);
     return v;
 }
 
-template <int ES>
-__device__ __forceinline__ float load_value(const char *p, int i)
+// Sum over groups of LG lanes, in every lane.
+template <int LG>
+__device__ __forceinline__ float group_sum(float v)
 {
-    return ES == 2 ? __uint_as_float((unsigned int)reinterpret_cast<const unsigned short *>(p)[i] << 16) : reinterpret_cast<const float *>(p)[i];
+    v += dpp_move<0xB1, 0xf>(v);                             // quad_perm [1,0,3,2]
+    v += dpp_move<0x4E, 0xf>(v);                             // quad_perm [2,3,0,1]
+    if (LG >= 8) v += dpp_move<0x141, 0xf>(v);               // row_half_mirror
+    if (LG >= 16) v += dpp_move<0x140, 0xf>(v);              // row_mirror
+    if (LG >= 32) v += __shfl_xor(v, 16);
+    return v;
 }
 
-// LG lanes a row.  PAIRS: neighbouring values turn together; otherwise i and i + R/2, whose chunks face each other (FACE) or not.
+// A rotated value is r (x_i w_i cos + x_j w_j (+-sin)), j its partner and r the norm's factor: two coefficients for every value of a lane,
+// the same for all query heads of a token, and for all key heads.
+// LG lanes a row, two 16-byte chunks each.  FACE (halves, R/2 whole chunks): the two that turn into each other, so that each angle is
+// computed once; otherwise neighbours.  PAIRS: neighbouring values turn together.  Neither: halves that begin inside a chunk; partners
+// are loaded one by one.
 template <int ES, int LG, bool PAIRS, bool FACE>
 __global__ void __launch_bounds__(256)
 k_qk_rope(const RopeArgs a)
@@ -49,32 +58,72 @@ k_qk_rope(const RopeArgs a)
     constexpr int E = 16 / ES;
     const int item = blockIdx.x * (256 / LG) + (int)threadIdx.x / LG;
     if (item >= a.tokens * a.slabs) return;                  // (whole groups leave)
-    const int c = threadIdx.x % LG, i0 = c * E;              // this lane's values: i0 .. i0 + E - 1
+    const int p = threadIdx.x % LG, half = a.R / 2;
+    int ch[2] = {2 * p, 2 * p + 1};                          // this lane's chunks: values ch * E on
+    if (FACE) {
+        const int hc = half / E;
+        ch[0] = p < hc ? p : 2 * p;
+        ch[1] = p < hc ? p + hc : 2 * p + 1;
+    }
     const int token = item / a.slabs, slab = item - token * a.slabs;
     const int b = token / a.T, t = token - b * a.T;
     const int pos = a.positions[token];
-    const bool mine = i0 < a.D;
+    const bool mine[2] = {ch[0] * E < a.D, ch[1] * E < a.D};
+    auto partner = [&](int i) { return PAIRS ? i ^ 1 : i < half ? i + half : i - half; };
 
-    // cosines and sines of this lane's values; a value outside the rotated part turns by nothing
-    float cs[E], sn[E];
-    int face = i0;                                           // first value of the chunk that this one pairs with
+    // the turns of a chunk's values, as vectors where the chunk turns as a whole
+    constexpr int FT = PAIRS ? E / 2 : E;
+    unsigned long long f[2][FT];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        cs[e] = 1.0f;
-        sn[e] = 0.0f;
-        const int i = i0 + e, half = a.R / 2;
-        if (i >= a.R || pos < 0) continue;
-        const int pair = PAIRS ? i / 2 : (i < half ? i : i - half);
-        const bool second = PAIRS ? (i & 1) : i >= half;
-        const unsigned int top = (unsigned int)(((unsigned long long)(unsigned int)pos * a.turns[pair]) >> 32);
-        const float turn = (float)(int)top * 0x1p-32f;       // [-1/2, 1/2]
-        float s, co;
-        sincospif(2.0f * turn, &s, &co);
-        cs[e] = a.magnitude * co;
-        sn[e] = a.magnitude * (second ? s : -s);             // partner's factor
+    for (int k = 0; k < (FACE ? 1 : 2); ++k) {
+        const int i0 = ch[k] * E;
+        if ((FACE || PAIRS) && i0 + E <= a.R) {
+            const ulonglong2 *from = reinterpret_cast<const ulonglong2 *>(a.turns + (PAIRS ? i0 / 2 : i0));
+#pragma unroll
+            for (int e = 0; e < FT; e += 2) {
+                const ulonglong2 two = from[e / 2];
+                f[k][e] = two.x;
+                f[k][e + 1] = two.y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < FT; ++e) {
+                const int i = i0 + (PAIRS ? 2 * e : e);
+                f[k][e] = i < a.R ? a.turns[PAIRS ? i / 2 : i < half ? i : i - half] : 0;
+            }
+        }
     }
-    const bool turned = i0 < a.R;
-    if (!PAIRS && FACE && turned) face = i0 < a.R / 2 ? i0 + a.R / 2 : i0 - a.R / 2;
+    float cs[2][E], sn[2][E];                                // a value outside the rotated part turns by nothing
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (FACE && k == 1) {                            // the same angles, the other sign
+                cs[1][e] = cs[0][e];
+                sn[1][e] = -sn[0][e];
+                continue;
+            }
+            if (PAIRS && (e & 1)) {
+                cs[k][e] = cs[k][e - 1];
+                sn[k][e] = -sn[k][e - 1];
+                continue;
+            }
+            cs[k][e] = 1.0f;
+            sn[k][e] = 0.0f;
+            const int i = ch[k] * E + e;
+            if (i >= a.R || pos < 0) continue;
+            const unsigned long long fi = f[k][PAIRS ? e / 2 : e];
+            const unsigned int top = __umulhi((unsigned int)pos, (unsigned int)fi) + (unsigned int)pos * (unsigned int)(fi >> 32);
+            const float turn = (float)(int)top * 0x1p-32f;   // [-1/2, 1/2]
+            float s, co;
+            if (ES == 2) {                                   // the hardware's functions take turns; off by 2^-20, a bf16 by 2^-9
+                s = __builtin_amdgcn_sinf(turn);
+                co = __builtin_amdgcn_cosf(turn);
+            } else
+                sincospif(2.0f * turn, &s, &co);
+            cs[k][e] = a.magnitude * co;
+            sn[k][e] = a.magnitude * (!PAIRS && i >= half ? s : -s);
+        }
 
     int64_t slot = -1;
     if (a.Hk && pos >= 0) {
@@ -83,76 +132,105 @@ k_qk_rope(const RopeArgs a)
         if (slot >= a.capacity) slot = -1;
     }
 
-    const int heads = a.Hq + 2 * a.Hk;
-    for (int h = slab; h < heads; h += a.slabs) {
-        const char *src;
-        char *dst;
-        const char *w;
-        const bool value = h >= a.Hq + a.Hk;
-        if (h < a.Hq) {
-            src = a.q + b * a.q_s[0] + t * a.q_s[1] + h * a.q_s[2];
-            dst = a.q_out + b * a.o_s[0] + t * a.o_s[1] + h * a.o_s[2];
-            w = (const char *)a.qw;
-        } else {
-            if (slot < 0) break;
-            const int hk = value ? h - a.Hq - a.Hk : h - a.Hq;
-            src = value ? a.v + b * a.v_s[0] + t * a.v_s[1] + hk * a.v_s[2] : a.k + b * a.k_s[0] + t * a.k_s[1] + hk * a.k_s[2];
-            dst = (value ? a.vc : a.kc) + b * a.c_s[0] + slot * a.c_s[1] + hk * a.c_s[2];
-            w = (const char *)a.kw;
-        }
-        u32x4 raw = {0, 0, 0, 0};
-        if (mine) raw = *reinterpret_cast<const u32x4 *>(src + c * 16);
-        if (value) {                                         // values go to the cache as they are
-            if (mine) *reinterpret_cast<u32x4 *>(dst + c * 16) = raw;
-            continue;
-        }
-        if (pos < 0) {                                       // padding: a query of zeros
-            if (mine) *reinterpret_cast<u32x4 *>(dst + c * 16) = u32x4{0, 0, 0, 0};
-            continue;
-        }
-        float x[E], y[E];                                    // own values, and those that they pair with
-        unpack_row16(raw, x);
-        if (PAIRS) {
+    // Heads first, first + slabs, .. below n, two at once (their loads are in flight together), with the coefficients u and v.
+    constexpr int N = 2;
+    auto turn_heads = [&](const char *src, int64_t src_h, char *dst, int64_t dst_h, int first, int n, const float (&u)[2][E], const float (&v)[2][E]) {
+        for (int h = first; h < n; h += N * a.slabs) {
+            u32x4 raw[N][2];
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = x[e ^ 1];
-        } else if (FACE) {
-            u32x4 other = raw;
-            if (turned && mine) other = *reinterpret_cast<const u32x4 *>(src + face * ES);
-            unpack_row16(other, y);
-        } else {
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = i0 + e, half = a.R / 2;
-                y[e] = mine && i < a.R ? load_value<ES>(src, i < half ? i + half : i - half) : x[e];
-            }
-        }
-        if (a.norm) {
-            float ss = 0.0f;
+                for (int k = 0; k < 2; ++k) {
+                    raw[j][k] = u32x4{0, 0, 0, 0};
+                    if (mine[k] && h + j * a.slabs < n) raw[j][k] = *reinterpret_cast<const u32x4 *>(src + (h + j * a.slabs) * src_h + ch[k] * 16);
+                }
 #pragma unroll
-            for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
+            for (int j = 0; j < N; ++j) {
+                const int hj = h + j * a.slabs;
+                if (hj >= n) break;
+                float x[2][E], y[2][E];                      // own values, and those that they pair with
 #pragma unroll
-            for (int o = LG / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
-            const float r = 1.0f / sqrtf(ss / (float)a.D + a.eps);
+                for (int k = 0; k < 2; ++k) unpack_row16(raw[j][k], x[k]);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                x[e] *= r;
-                y[e] *= r;
-            }
-            if (w && mine) {
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int i = i0 + e, half = a.R / 2;
-                    const int p = i >= a.R ? i : PAIRS ? i ^ 1 : i < half ? i + half : i - half;
-                    x[e] *= load_value<ES>(w, i) + a.offset;
-                    y[e] *= load_value<ES>(w, p) + a.offset;
+                    for (int e = 0; e < E; ++e) {
+                        const int i = ch[k] * E + e;
+                        y[k][e] = PAIRS ? x[k][e ^ 1] : FACE ? x[1 - k][e] : i < a.R ? attn_value<ES>(src + hj * src_h, partner(i)) : 0.0f;
+                    }
+                float r = 1.0f;
+                if (a.norm) {
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) ss = fmaf(x[k][e], x[k][e], ss);
+                    r = __builtin_amdgcn_rsqf(fmaf(group_sum<LG>(ss), a.inv_d, a.eps));
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float z[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        // (what does not turn meets no other value)
+                        z[e] = ch[k] * E + e < a.R ? fmaf(x[k][e], u[k][e], y[k][e] * v[k][e]) : x[k][e] * u[k][e];
+                        if (a.norm) z[e] *= r;
+                    }
+                    if (mine[k]) *reinterpret_cast<u32x4 *>(dst + hj * dst_h + ch[k] * 16) = pack_row16<ES>(z);
                 }
             }
         }
+    };
+    auto coefficients = [&](const char *w, float (&u)[2][E], float (&v)[2][E]) {
+        float own[2][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (i0 + e < a.R) x[e] = fmaf(x[e], cs[e], y[e] * sn[e]);
-        if (mine) *reinterpret_cast<u32x4 *>(dst + c * 16) = pack_row16<ES>(x);
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) own[k][e] = 1.0f;
+        const bool scaled = a.norm && w;
+        if (scaled) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (!mine[k]) continue;
+                unpack_row16(*reinterpret_cast<const u32x4 *>(w + ch[k] * 16), own[k]);
+#pragma unroll
+                for (int e = 0; e < E; ++e) own[k][e] += a.offset;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int i = ch[k] * E + e;
+                u[k][e] = cs[k][e] * own[k][e];
+                v[k][e] = sn[k][e] * (PAIRS ? own[k][e ^ 1] : FACE ? own[1 - k][e] : scaled && i < a.R ? attn_value<ES>(w, partner(i)) + a.offset : 1.0f);
+            }
+    };
+
+    float u[2][E], v[2][E];
+    if (slab < a.Hq) {
+        const char *src = a.q + b * a.q_s[0] + t * a.q_s[1];
+        char *dst = a.q_out + b * a.o_s[0] + t * a.o_s[1];
+        if (pos < 0) {                                       // padding: queries of zeros
+            for (int h = slab; h < a.Hq; h += a.slabs)
+                for (int k = 0; k < 2; ++k)
+                    if (mine[k]) *reinterpret_cast<u32x4 *>(dst + h * a.o_s[2] + ch[k] * 16) = u32x4{0, 0, 0, 0};
+            return;
+        }
+        coefficients((const char *)a.qw, u, v);
+        turn_heads(src, a.q_s[2], dst, a.o_s[2], slab, a.Hq, u, v);
     }
+    if (slot < 0) return;
+    const int k0 = (slab + a.slabs - a.Hq % a.slabs) % a.slabs, v0 = (slab + a.slabs - (a.Hq + a.Hk) % a.slabs) % a.slabs;
+    char *kc = a.kc + b * a.c_s[0] + slot * a.c_s[1], *vc = a.vc + b * a.c_s[0] + slot * a.c_s[1];
+    if (k0 < a.Hk) {
+        coefficients((const char *)a.kw, u, v);
+        turn_heads(a.k + b * a.k_s[0] + t * a.k_s[1], a.k_s[2], kc, a.c_s[2], k0, a.Hk, u, v);
+    }
+    const char *vs = a.v + b * a.v_s[0] + t * a.v_s[1];
+    for (int h = v0; h < a.Hk; h += a.slabs)                 // values go to the cache as they are
+        for (int k = 0; k < 2; ++k)
+            if (mine[k]) *reinterpret_cast<u32x4 *>(vc + h * a.c_s[2] + ch[k] * 16) = *reinterpret_cast<const u32x4 *>(vs + h * a.v_s[2] + ch[k] * 16);
 }
 
 template <int ES, int LG>
@@ -226,9 +304,8 @@ extern "C" clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, co
     if (rope->layout != CLADA_ROPE_HALF && rope->layout != CLADA_ROPE_PAIRS) return clada_fail(ctx, CLADA_ERR_VALUE, "unknown rotary layout %d", (int)rope->layout);
     if (!isfinite(rope->magnitude)) return clada_fail(ctx, CLADA_ERR_VALUE, "magnitude is not finite");
     if (norm && (!(norm->eps >= 0.0f) || !isfinite(norm->eps) || !isfinite(norm->offset))) return clada_fail(ctx, CLADA_ERR_VALUE, "eps or offset out of range");
-    if (((uintptr_t)rope->turns & 7u) || ((uintptr_t)positions & 3u) || ((uintptr_t)slots & 3u) ||
-        (norm && (((uintptr_t)norm->q_weight | (uintptr_t)norm->k_weight) & (dtype_size(cache->dtype) - 1))))
-        return clada_fail(ctx, CLADA_ERR_ALIGN, "an array is not aligned to its type");
+    if ((((uintptr_t)positions | (uintptr_t)slots) & 3u) || !aligned16(rope->turns) || (norm && (!aligned16(norm->q_weight) || !aligned16(norm->k_weight))))
+        return clada_fail(ctx, CLADA_ERR_ALIGN, "turns and weights must be 16-byte, positions and slots 4-byte aligned");
     if (q && (st = clada_check_heads(ctx, q, cache->dtype, "q")) != CLADA_OK) return st;
     if (q && (st = clada_check_heads(ctx, q_out, cache->dtype, "q_out")) != CLADA_OK) return st;
     if (k && (st = clada_check_heads(ctx, k, cache->dtype, "k")) != CLADA_OK) return st;
@@ -269,6 +346,7 @@ extern "C" clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, co
     a.n_sink = cache->n_sink;
     a.ring = cache->ring;
     a.magnitude = rope->magnitude;
+    a.inv_d = 1.0f / (float)cache->d;
     if (norm) {
         a.norm = 1;
         a.qw = norm->q_weight;
@@ -276,24 +354,24 @@ extern "C" clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, co
         a.eps = norm->eps;
         a.offset = norm->offset;
     }
-    // A group takes up to eight heads of a token once that leaves groups enough for the chip; fewer tokens spread over more groups.
-    const int heads = a.Hq + 2 * a.Hk, chunks = a.D * es / 16;
-    int lg = 8;
-    while (lg < chunks) lg *= 2;
+    // A group takes up to eight heads of a token where that leaves sixteen waves for every compute unit; fewer tokens spread over more groups.
+    const int heads = a.Hq + 2 * a.Hk, pairs_of_chunks = (a.D * es / 16 + 1) / 2;
+    int lg = 4;
+    while (lg < pairs_of_chunks) lg *= 2;
     int per = 8;
-    while (per > 1 && (int64_t)a.tokens * ((heads + per - 1) / per) * lg < (int64_t)ctx->num_cu * 2048) per /= 2;
+    while (per > 1 && (int64_t)a.tokens * ((heads + per - 1) / per) * lg < (int64_t)ctx->num_cu * 1024) per /= 2;
     a.slabs = (heads + per - 1) / per;
     const bool pairs = rope->layout == CLADA_ROPE_PAIRS;
     hipStream_t s = (hipStream_t)hip_stream;
     if (es == 2) {
-        if (lg == 8) launch_rope<2, 8>(a, pairs, s);
-        else if (lg == 16) launch_rope<2, 16>(a, pairs, s);
-        else launch_rope<2, 32>(a, pairs, s);
+        if (lg == 4) launch_rope<2, 4>(a, pairs, s);
+        else if (lg == 8) launch_rope<2, 8>(a, pairs, s);
+        else launch_rope<2, 16>(a, pairs, s);
     } else {
-        if (lg == 8) launch_rope<4, 8>(a, pairs, s);
+        if (lg == 4) launch_rope<4, 4>(a, pairs, s);
+        else if (lg == 8) launch_rope<4, 8>(a, pairs, s);
         else if (lg == 16) launch_rope<4, 16>(a, pairs, s);
-        else if (lg == 32) launch_rope<4, 32>(a, pairs, s);
-        else launch_rope<4, 64>(a, pairs, s);
+        else launch_rope<4, 32>(a, pairs, s);
     }
     CLADA_CHECK_HIP(ctx, hipGetLastError());
     return CLADA_OK;
