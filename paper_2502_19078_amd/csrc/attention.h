@@ -29,9 +29,9 @@ struct AttnArgs {
     float *part_o;
 };
 
-// Which kernel: tiles of 16 rows (both types), 32 rows (fp32), 128 rows (bf16); a shared prefix in tiles of 128 rows with the
-// sequences' own keys in tiles of 16 (bf16).  Partial results are joined where there are any.
-enum AttnPath { ATTN_ROWS16, ATTN_ROWS32, ATTN_TILES, ATTN_PREFIX };
+// Which kernel: tiles of 16 rows, of 128 rows, or a shared prefix in tiles of 128 rows with the sequences' own keys in tiles of 16.  Partial
+// results are joined where there are any.
+enum AttnPath { ATTN_ROWS, ATTN_TILES, ATTN_PREFIX };
 hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, hipStream_t stream);
 
 #ifdef __HIPCC__

@@ -7,33 +7,33 @@
 
 namespace {
 
-template <int ES, int DP, int NT, bool FULL>
-__global__ void __launch_bounds__(256, ES == 2 && DP <= 128 ? 2 : 1)
+template <int ES, int DP, bool FULL>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_attn_rows(const AttnArgs a)
 {
-    __shared__ __align__(16) char lds[RowsShape<ES, DP, NT>::LDS];
+    __shared__ __align__(16) char lds[RowsShape<ES, DP>::LDS];
     const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
-    attn_rows<ES, DP, NT, FULL>(a, id < pre_blocks, id < pre_blocks ? id : id - pre_blocks, lds);
+    attn_rows<ES, DP, FULL>(a, id < pre_blocks, id < pre_blocks ? id : id - pre_blocks, lds);
 }
 
-template <int DP, bool FULL>
+template <int ES, int DP, bool FULL>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_attn_tiles(const AttnArgs a)
 {
-    __shared__ __align__(16) char lds[TilesShape<DP>::LDS];
-    attn_tiles<DP, FULL>(a, false, blockIdx.x, lds);
+    __shared__ __align__(16) char lds[TilesShape<ES, DP>::LDS];
+    attn_tiles<ES, DP, FULL>(a, false, blockIdx.x, lds);
 }
 
 // A shared prefix for more than 16 rows: its workgroups first, then those of the sequences' own keys, in one launch.
-template <int DP, bool FULL>
+template <int ES, int DP, bool FULL>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_attn_prefix(const AttnArgs a)
 {
-    constexpr int L0 = TilesShape<DP>::LDS, L1 = RowsShape<2, DP, 1>::LDS;
+    constexpr int L0 = TilesShape<ES, DP>::LDS, L1 = RowsShape<ES, DP>::LDS;
     __shared__ __align__(16) char lds[L0 > L1 ? L0 : L1];
     const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
-    if (id < pre_blocks) attn_tiles<DP, FULL>(a, true, id, lds);
-    else attn_rows<2, DP, 1, FULL>(a, false, id - pre_blocks, lds);
+    if (id < pre_blocks) attn_tiles<ES, DP, FULL>(a, true, id, lds);
+    else attn_rows<ES, DP, FULL>(a, false, id - pre_blocks, lds);
 }
 
 // One workgroup a row: its splits' partial results joined in a fixed order.  TPR threads hold 4 values each of a row; the 256 / TPR groups take
@@ -94,29 +94,30 @@ k_attn_join(const AttnArgs a)
         *reinterpret_cast<f32x4 *>(to + dim * 4) = o;
 }
 
-template <int ES, int DP, int NT>
-void launch_rows(const AttnArgs &a, dim3 grid, hipStream_t stream)
+template <int ES, int DP, bool FULL>
+void launch_full(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
 {
-    if (a.D == DP) hipLaunchKernelGGL((k_attn_rows<ES, DP, NT, true>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((k_attn_rows<ES, DP, NT, false>), grid, dim3(256), 0, stream, a);
+    if (path == ATTN_TILES) hipLaunchKernelGGL((k_attn_tiles<ES, DP, FULL>), grid, dim3(256), 0, stream, a);
+    if constexpr (ES == 2 || DP % 64 == 0) {                 // (the rows of the fp32 kernels come in 64 values)
+        if (path == ATTN_ROWS) hipLaunchKernelGGL((k_attn_rows<ES, DP, FULL>), grid, dim3(256), 0, stream, a);
+        if (path == ATTN_PREFIX) hipLaunchKernelGGL((k_attn_prefix<ES, DP, FULL>), grid, dim3(256), 0, stream, a);
+    }
 }
 
-template <int DP>
-void launch_bf16(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
+template <int ES, int DP>
+void launch(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
 {
-    const bool full = a.D == DP;
-    if (path == ATTN_ROWS16) launch_rows<2, DP, 1>(a, grid, stream);
-    else if (path == ATTN_TILES && full) hipLaunchKernelGGL((k_attn_tiles<DP, true>), grid, dim3(256), 0, stream, a);
-    else if (path == ATTN_TILES) hipLaunchKernelGGL((k_attn_tiles<DP, false>), grid, dim3(256), 0, stream, a);
-    else if (full) hipLaunchKernelGGL((k_attn_prefix<DP, true>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((k_attn_prefix<DP, false>), grid, dim3(256), 0, stream, a);
+    if (a.D == DP) launch_full<ES, DP, true>(a, path, grid, stream);
+    else launch_full<ES, DP, false>(a, path, grid, stream);
 }
 
-template <int DP>
-void launch_f32(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
+template <int ES>
+void launch_type(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
 {
-    if (path == ATTN_ROWS16) launch_rows<4, DP, 1>(a, grid, stream);
-    else launch_rows<4, DP, 2>(a, grid, stream);
+    if (a.D <= 64) launch<ES, 64>(a, path, grid, stream);
+    else if (a.D <= 96 && (ES == 2 || path == ATTN_TILES)) launch<ES, 96>(a, path, grid, stream);
+    else if (a.D <= 128) launch<ES, 128>(a, path, grid, stream);
+    else launch<ES, 256>(a, path, grid, stream);
 }
 
 }  // namespace
@@ -124,16 +125,8 @@ void launch_f32(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
 hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, hipStream_t stream)
 {
     const dim3 grid((unsigned int)((int64_t)a.Hkv * a.pre_tiles * a.pre_splits + (int64_t)a.B * a.Hkv * a.own_tiles * a.splits));
-    if (es == 2) {
-        if (a.D <= 64) launch_bf16<64>(a, path, grid, stream);
-        else if (a.D <= 96) launch_bf16<96>(a, path, grid, stream);
-        else if (a.D <= 128) launch_bf16<128>(a, path, grid, stream);
-        else launch_bf16<256>(a, path, grid, stream);
-    } else {
-        if (a.D <= 64) launch_f32<64>(a, path, grid, stream);
-        else if (a.D <= 128) launch_f32<128>(a, path, grid, stream);
-        else launch_f32<256>(a, path, grid, stream);
-    }
+    if (es == 2) launch_type<2>(a, path, grid, stream);
+    else launch_type<4>(a, path, grid, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits + a.pre_splits == 1) return e;
     const dim3 rows((unsigned int)((int64_t)a.B * a.T * a.Hq)), block(256);

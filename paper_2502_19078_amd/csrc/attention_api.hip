@@ -139,8 +139,8 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     a.window = window;
     a.sinks = window ? sinks : 0;
     const int es = (int)dtype_size(cache->dtype);
-    const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS16 : es == 2 ? ATTN_TILES : ATTN_ROWS32;
-    const int tile = path == ATTN_ROWS16 ? 16 : path == ATTN_ROWS32 ? 32 : 128;
+    const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
+    const int tile = path == ATTN_ROWS ? 16 : 128;
     a.own_tiles = (T * a.G + tile - 1) / tile;
     const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
     int64_t keys = cache->capacity;                          // what a tile can see at most
@@ -179,10 +179,10 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     a.pre = kv_of(prefix);
     a.pre_n = prefix_len;
     const int es = (int)dtype_size(cache->dtype);
-    const AttnPath path = B * a.G <= 16 ? ATTN_ROWS16 : es == 2 ? ATTN_PREFIX : ATTN_ROWS32;
-    const int tile = path == ATTN_ROWS16 ? 16 : path == ATTN_ROWS32 ? 32 : 128, own = path == ATTN_ROWS32 ? 32 : 16;
+    const AttnPath path = B * a.G <= 16 ? ATTN_ROWS : ATTN_PREFIX;
+    const int tile = path == ATTN_ROWS ? 16 : 128;
     a.pre_tiles = (B * a.G + tile - 1) / tile;
-    a.own_tiles = (a.G + own - 1) / own;
+    a.own_tiles = (a.G + 15) / 16;
     a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
     a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
     if ((st = place_parts(ctx, a)) != CLADA_OK) return st;

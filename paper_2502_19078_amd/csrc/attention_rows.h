@@ -4,7 +4,7 @@
 // One pass over the keys with a running maximum and sum per row, in base 2.
 //
 // Bound by the cache's bytes (HBM): a key head's rows of the cache are read once for all query heads of its group.  A workgroup takes a tile
-// of 16 or 32 rows and one split of their keys; its four waves take 32 (fp32: 16) keys in turn, each with a running softmax of its own, so
+// of 16 rows and one split of their keys; its four waves take 32 (fp32: 16) keys in turn, each with a running softmax of its own, so
 // nothing waits inside the loop; the waves' results are joined through LDS, those of the splits by k_attn_join.
 //
 // Scores are formed transposed, S^T = K Q^T: a lane then holds scores of one row only, keys 4 (lane / 16) + i of each 16, and the same
@@ -16,25 +16,26 @@
 
 namespace {
 
-// ES: bytes a value.  DP: D rounded up to the products' tiles; FULL: D == DP.  NT: tiles of 16 rows.
-template <int ES, int DP, int NT>
+// ES: bytes a value.  DP: D rounded up to the products' tiles; FULL: D == DP.
+template <int ES, int DP>
 struct RowsShape {
     static constexpr int KB = ES == 2 ? 2 : 1, KS = 16 * KB; // keys of a step
     static constexpr int PITCH = DP * 2 + 32;                // V in LDS: rows 8 banks apart modulo 64
-    static constexpr int V_LDS = ES == 2 ? 4 * 32 * PITCH : 0, J_LDS = DP * 256 + 512 * NT + 16;     // of the join: outputs and maxima of four waves
+    static constexpr int V_LDS = ES == 2 ? 4 * 32 * PITCH : 0, J_LDS = DP * 256 + 512 + 16;     // of the join: outputs and maxima of four waves
     static constexpr int LDS = V_LDS > J_LDS ? V_LDS : J_LDS;
 };
 
-template <int ES, int DP, int NT, bool FULL>
+template <int ES, int DP, bool FULL>
 __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, const int block, char *lds)
 {
-    using S = RowsShape<ES, DP, NT>;
+    using S = RowsShape<ES, DP>;
     constexpr int CH = DP * ES / 64;                         // chunks of 64 bytes in a row: lane group g holds 16 bytes of each
     constexpr int KB = S::KB, KS = S::KS, PITCH = S::PITCH;
     constexpr int DB = DP / 16;                              // tiles of 16 output dimensions
     constexpr int CPR = DP * ES / 16;                        // 16-byte chunks of a row
     constexpr int VL = KS * CPR / 64;                        // 16-byte loads of V a lane and step
 
+    static_assert(ES == 2 || DP % 64 == 0, "whole loads of V");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g = lane >> 4;
     const int Dd = FULL ? DP : a.D;
@@ -59,26 +60,20 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
         rows = a.T * a.G;
     }
     const int all_splits = a.splits + a.pre_splits, part = pre ? split : a.pre_splits + split;
-    const int r0 = tile * 16 * NT;
+    const int r0 = tile * 16;
     const AttnKV &kv = pre ? a.pre : a.kv;
 
-    // this lane's rows: queries as the second operand.  (Loaded ahead of the lengths, which the keys wait for.)
+    // this lane's row: its query as the second operand.  (Loaded ahead of the lengths, which the keys wait for.)
     const int len_b = pre ? 0 : a.lens[b], qlen_b = pre || !a.q_lens ? a.T : a.q_lens[b];
-    u32x4 qf[NT][CH];
-    int row_pos[NT];
-    RowAt at[NT];
+    u32x4 qf[CH];
+    const int row = min(r0 + n16, rows - 1), token = !pre && a.T == 1 ? 0 : row / a.G;
+    const RowAt at = row_at(a, pre, b, h, row, token);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = min(r0 + nt * 16 + n16, rows - 1);
-        row_pos[nt] = !pre && a.T == 1 ? 0 : r / a.G;        // (the row's token for now)
-        at[nt] = row_at(a, pre, b, h, r, row_pos[nt]);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int off = 64 * c + 16 * g;
-            const bool in = FULL || off < Dd * ES;
-            qf[nt][c] = *reinterpret_cast<const u32x4 *>(a.q + at[nt].q + (in ? off : 0));
-            if (!in) qf[nt][c] = u32x4{0, 0, 0, 0};
-        }
+    for (int c = 0; c < CH; ++c) {
+        const int off = 64 * c + 16 * g;
+        const bool in = FULL || off < Dd * ES;
+        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + at.q + (in ? off : 0));
+        if (!in) qf[c] = u32x4{0, 0, 0, 0};
     }
     KeyRange kr;
     int first_pos = 0, qlen = a.T;
@@ -95,10 +90,9 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
         else if (a.T == 1)
             kr = key_range(kv, first_pos, 0, qlen - 1, a.window, a.sinks);
         else
-            kr = key_range(kv, first_pos, r0 / a.G, min(min(r0 + 16 * NT - 1, rows - 1) / a.G, qlen - 1), a.window, a.sinks);
+            kr = key_range(kv, first_pos, r0 / a.G, min(min(r0 + 15, rows - 1) / a.G, qlen - 1), a.window, a.sinks);
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) row_pos[nt] = pre || a.pre_splits ? 0 : row_pos[nt] < qlen ? first_pos + row_pos[nt] : -1;
+    const int row_pos = pre || a.pre_splits ? 0 : token < qlen ? first_pos + token : -1;
     const bool one_pos = pre || a.pre_splits || kr.pos_a == kr.pos_b;      // all rows see the same keys
     int chunk = (kr.n + splits - 1) / splits;
     chunk = (chunk + 31) & ~31;
@@ -107,10 +101,12 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
     const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
     char *my_v = lds + wave * 32 * PITCH;
 
-    f32x4 o[NT][DB];
-    float m[NT], l[NT];
+    f32x4 o[DB];
+    float m = NEG_INF, l = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = f32x4{0, 0, 0, 0};
     u32x4 kf[KB][CH], vf[VL];
-    auto load = [&](int i) {                                 // keys i .. i + KS - 1; past the end the last one again
+    auto load_k = [&](int i) {                               // keys i .. i + KS - 1; past the end the last one again
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             const char *p = kp + kr.row(kr.pos(min(i + kb * 16 + n16, k1 - 1)), kv) * kv.sn;
@@ -122,9 +118,11 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
                 if (!in) kf[kb][c] = u32x4{0, 0, 0, 0};
             }
         }
+    };
+    auto load_v = [&](int i) {
 #pragma unroll
         for (int j = 0; j < VL; ++j) {
-            int key, col;                                    // bf16: chunks in order of the rows, for LDS; fp32: key 4 g + i, 64 values a load
+            int key, col;                                    // bf16: chunks in order of the rows, for LDS; fp32: key 4 g + j % 4, 64 values a load
             if (ES == 2) {
                 const int id = lane + 64 * j;
                 key = id / CPR;
@@ -140,36 +138,29 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
         }
     };
 
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = NEG_INF;
-        l[nt] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[nt][d] = f32x4{0, 0, 0, 0};
-    }
     int i = k0 + wave * KS;
-    if (i < k1) load(i);
+    if (i < k1) {
+        load_k(i);
+        load_v(i);
+    }
     for (; i < k1; i += 4 * KS) {
         // scores of KS keys: lane holds keys 16 kb + 4 g + e of its row
-        f32x4 s[NT][KB];
+        f32x4 s[KB];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int kb = 0; kb < KB; ++kb) {
+            s[kb] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                s[nt][kb] = f32x4{0, 0, 0, 0};
+            for (int c = 0; c < CH; ++c) {
+                if (ES == 2)
+                    s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[kb][c]), __builtin_bit_cast(bf16x8, qf[c]), s[kb], 0, 0, 0);
+                else
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    if (ES == 2)
-                        s[nt][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[kb][c]),
-                                                                            __builtin_bit_cast(bf16x8, qf[nt][c]), s[nt][kb], 0, 0, 0);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const unsigned int ka = kf[kb][c][e], qb = qf[nt][c][e];
-                            s[nt][kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(ka), __uint_as_float(qb), s[nt][kb], 0, 0, 0);
-                        }
-                }
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned int ka = kf[kb][c][e], qb = qf[c][e];
+                        s[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(ka), __uint_as_float(qb), s[kb], 0, 0, 0);
+                    }
             }
+        }
         const int p_first = kr.pos(i), p_last = kr.pos(min(i + KS, k1) - 1);
         const bool mixed = !one_pos && !(p_last <= kr.pos_a && (a.window == 0 || p_first > kr.pos_b - a.window || p_last < a.sinks));
         if (ES == 2) {
@@ -179,168 +170,153 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
                 *reinterpret_cast<u32x4 *>(my_v + id / CPR * PITCH + id % CPR * 16) = vf[j];
             }
         }
-        u32x4 va[ES == 4 ? VL : 1];
-        if (ES == 4)
-#pragma unroll
-            for (int j = 0; j < VL; ++j) va[ES == 4 ? j : 0] = vf[j];
         const int next = i + 4 * KS;
-        if (next < k1) load(next);
+        if (next < k1) {
+            load_k(next);
+            if (ES == 2) load_v(next);                       // (in LDS by now)
+        }
         __builtin_amdgcn_wave_barrier();
 
+        float top = NEG_INF;
+        const Sight see = sight(kr, i + 4 * g, k1, row_pos, a.window, a.sinks);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float top = NEG_INF;
-            const Sight see = sight(kr, i + 4 * g, k1, row_pos[nt], a.window, a.sinks);
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = kb * 16 + e;
-                    float x = s[nt][kb][e] * a.scale2;
-                    const bool seen = mixed ? see(key) : key < see.end;
-                    x = seen ? x : NEG_INF;
-                    s[nt][kb][e] = x;
-                    top = fmaxf(top, x);
-                }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (__any(top > m[nt])) {
-                const float mn = fmaxf(m[nt], top);
-                const float f = mn == NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - mn);
-                m[nt] = mn;
-                l[nt] *= f;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[nt][d] *= f;
+            for (int e = 0; e < 4; ++e) {
+                const int key = kb * 16 + e;
+                float x = s[kb][e] * a.scale2;
+                const bool seen = mixed ? see(key) : key < see.end;
+                x = seen ? x : NEG_INF;
+                s[kb][e] = x;
+                top = fmaxf(top, x);
             }
-            const float base = m[nt] == NEG_INF ? 0.0f : m[nt];
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m + 8.0f)) {                         // (weights up to 2^8 lose nothing)
+            const float mn = top > m + 8.0f ? top : m;
+            const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(s[nt][kb][e] - base);
-                    s[nt][kb][e] = p;
-                    l[nt] += p;
-                }
+            for (int d = 0; d < DB; ++d) o[d] *= f;
         }
+        const float base = m == NEG_INF ? 0.0f : m;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(s[kb][e] - base);
+                s[kb][e] = p;
+                l += p;
+            }
 
         if (ES == 2) {
-            u32x4 hi[NT], lo[NT];
+            u32x4 hi, lo;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float p0 = s[nt][(w >> 1) % KB][2 * (w & 1)], p1 = s[nt][(w >> 1) % KB][2 * (w & 1) + 1];
-                    const unsigned int u = pack_bf16(p0, p1);
-                    hi[nt][w] = u;
-                    lo[nt][w] = pack_bf16(p0 - __uint_as_float(u << 16), p1 - __uint_as_float(u & 0xffff0000u));
-                }
+            for (int w = 0; w < 4; ++w) {
+                const float p0 = s[(w >> 1) % KB][2 * (w & 1)], p1 = s[(w >> 1) % KB][2 * (w & 1) + 1];
+                const unsigned int u = pack_bf16(p0, p1);
+                hi[w] = u;
+                lo[w] = pack_bf16(p0 - __uint_as_float(u << 16), p1 - __uint_as_float(u & 0xffff0000u));
+            }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const char *src = my_v + (4 * g + (n16 >> 2)) * PITCH + d * 32 + (n16 & 3) * 8;
                 const uint2 u0 = read_tr16(src), u1 = read_tr16(src + 16 * PITCH);
                 const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y});
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    o[nt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, hi[nt]), o[nt][d], 0, 0, 0);
-                    o[nt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, lo[nt]), o[nt][d], 0, 0, 0);
-                }
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, hi), o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, lo), o[d], 0, 0, 0);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < VL; ++j)                     // keys 4 g + j % 4, dimensions 64 (j / 4) + 4 n16 + e
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const unsigned int vv = va[ES == 4 ? j : 0][e];
-                        o[nt][(j / 4 * 4 + e) % DB] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vv), s[nt][0][j % 4], o[nt][(j / 4 * 4 + e) % DB], 0, 0, 0);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned int vv = vf[j][e];
+                    f32x4 &to = o[(j / 4 * 4 + e) % DB];
+                    to = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vv), s[0][j % 4], to, 0, 0, 0);
+                }
+            if (next < k1) load_v(next);
         }
     }
 
-    // The waves' results side by side in LDS; then every wave joins a part of each row's outputs: v[nt][x] are the four from dim(x) on.
+    // The waves' results side by side in LDS; then every wave joins a part of each row's outputs: v[x] are the four from dim(x) on.
     constexpr int OUT = (DB + 3) / 4;
     auto dim = [&](int x) { return ES == 2 ? 16 * (wave + 4 * x) + 4 * g : 64 * x + 16 * g + 4 * wave; };
     float2 *s_ml = reinterpret_cast<float2 *>(lds + DP * 256);
-    unsigned int *s_again = reinterpret_cast<unsigned int *>(lds + DP * 256 + 512 * NT);
-    f32x4 v[NT][OUT];
+    unsigned int *s_again = reinterpret_cast<unsigned int *>(lds + DP * 256 + 512);
+    f32x4 v[OUT];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        l[nt] += __shfl_xor(l[nt], 16);
-        l[nt] += __shfl_xor(l[nt], 32);
-        __syncthreads();
+    for (int d = 0; d < DB; ++d) reinterpret_cast<f32x4 *>(lds)[(wave * DB + d) * 64 + lane] = o[d];
+    if (g == 0) s_ml[wave * 16 + n16] = make_float2(m, l);
+    if (threadIdx.x == 0) *s_again = 0;
+    __syncthreads();
+    float2 ml[4];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) reinterpret_cast<f32x4 *>(lds)[(wave * DB + d) * 64 + lane] = o[nt][d];
-        if (g == 0) s_ml[(wave * NT + nt) * 16 + n16] = make_float2(m[nt], l[nt]);
-        if (nt == 0 && threadIdx.x == 0) *s_again = 0;
-        __syncthreads();
-        float2 ml[4];
+    for (int w = 0; w < 4; ++w) ml[w] = s_ml[w * 16 + n16];
+    m = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+    l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) ml[w] = s_ml[(w * NT + nt) * 16 + n16];
-        m[nt] = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
-        l[nt] = 0.0f;
+    for (int x = 0; x < OUT; ++x) v[x] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int x = 0; x < OUT; ++x) v[nt][x] = f32x4{0, 0, 0, 0};
+    for (int w = 0; w < 4; ++w) {
+        const float f = ml[w].x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(ml[w].x - m);
+        l += ml[w].y * f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = ml[w].x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(ml[w].x - m[nt]);
-            l[nt] += ml[w].y * f;
+        for (int x = 0; x < OUT; ++x) {
+            if (ES == 2) {
+                if (DB % 4 == 0 || wave + 4 * x < DB) v[x] += reinterpret_cast<const f32x4 *>(lds)[(w * DB + wave + 4 * x) * 64 + lane] * f;
+            } else
 #pragma unroll
-            for (int x = 0; x < OUT; ++x) {
-                if (ES == 2) {
-                    if (DB % 4 == 0 || wave + 4 * x < DB) v[nt][x] += reinterpret_cast<const f32x4 *>(lds)[(w * DB + wave + 4 * x) * 64 + lane] * f;
-                } else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[nt][x][e] += reinterpret_cast<const float *>(lds)[((w * DB + 4 * x + e) * 64 + lane) * 4 + wave] * f;
-            }
+                for (int e = 0; e < 4; ++e) v[x][e] += reinterpret_cast<const float *>(lds)[((w * DB + 4 * x + e) * 64 + lane) * 4 + wave] * f;
         }
-        bool fine = l[nt] < INFINITY;
+    }
+    bool fine = l < INFINITY;
 #pragma unroll
-        for (int x = 0; x < OUT; ++x)
+    for (int x = 0; x < OUT; ++x)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) fine = fine && fabsf(v[nt][x][e]) < INFINITY;
-        unsigned long long odd = __ballot(!fine && !(l[nt] != l[nt]) && row_pos[nt] >= 0 && r0 + nt * 16 + n16 < rows);
-        if (odd) {
-            odd |= odd >> 32;
-            if (lane == 0) atomicOr(s_again, (unsigned int)((odd | odd >> 16) & 0xffff) << (nt * 16));
-        }
+        for (int e = 0; e < 4; ++e) fine = fine && fabsf(v[x][e]) < INFINITY;
+    unsigned long long odd = __ballot(!fine && !(l != l) && row_pos >= 0 && r0 + n16 < rows);
+    if (odd) {
+        odd |= odd >> 32;
+        if (lane == 0) atomicOr(s_again, (unsigned int)((odd | odd >> 16) & 0xffff));
     }
     __syncthreads();
     const unsigned int again = kr.n ? __builtin_amdgcn_readfirstlane(*s_again) : 0u;
     if (again) {
-        for (int t = wave; t < 16 * NT; t += 4) {
+        for (int t = wave; t < 16; t += 4) {
             if (!(again >> t & 1)) continue;
-            const int r = r0 + t;
-            const RowAt row = row_at(a, pre, b, h, r, r / a.G);
-            attn_store_again<ES>(a, attn_row_again<ES>(a, kr, kv, kp, vp, a.q + row.q, pre || a.pre_splits ? INT32_MAX : first_pos + r / a.G, k0, k1), row, part);
+            const int i = (r0 + t) / a.G;
+            const RowAt to = row_at(a, pre, b, h, r0 + t, i);
+            attn_store_again<ES>(a, attn_row_again<ES>(a, kr, kv, kp, vp, a.q + to.q, pre || a.pre_splits ? INT32_MAX : first_pos + i, k0, k1), to, part);
         }
     }
 
+    if (r0 + n16 >= rows || (again >> n16 & 1)) return;
+    if (all_splits > 1) {
+        const int64_t at_part = at.lse * all_splits + part;
+        if (g == 0 && wave == 0) a.part_ml[at_part] = make_float2(m, l);
+        if (k0 == k1) return;                                // nothing to read for this split
+        float *to = a.part_o + at_part * Dd;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        if (r0 + nt * 16 + n16 >= rows || (again >> (nt * 16 + n16) & 1)) continue;
-        if (all_splits > 1) {
-            const int64_t at_part = at[nt].lse * all_splits + part;
-            if (g == 0 && wave == 0) a.part_ml[at_part] = make_float2(m[nt], l[nt]);
-            if (k0 == k1) continue;                          // nothing to read for this split
-            float *to = a.part_o + at_part * Dd;
+        for (int x = 0; x < OUT; ++x)
+            if (dim(x) < Dd) *reinterpret_cast<f32x4 *>(to + dim(x)) = v[x];
+        return;
+    }
+    const bool none = kr.n == 0 || row_pos < 0;
+    if (a.lse && g == 0 && wave == 0) a.lse[at.lse] = none ? NEG_INF : (m == NEG_INF ? NEG_INF : m * 0.69314718055994531f) + logf(l);
+    const float inv = 1.0f / l;
 #pragma unroll
-            for (int x = 0; x < OUT; ++x)
-                if (dim(x) < Dd) *reinterpret_cast<f32x4 *>(to + dim(x)) = v[nt][x];
-            continue;
-        }
-        const bool none = kr.n == 0 || row_pos[nt] < 0;
-        if (a.lse && g == 0 && wave == 0) a.lse[at[nt].lse] = none ? NEG_INF : (m[nt] == NEG_INF ? NEG_INF : m[nt] * 0.69314718055994531f) + logf(l[nt]);
-        const float inv = 1.0f / l[nt];
-#pragma unroll
-        for (int x = 0; x < OUT; ++x) {
-            if (dim(x) >= Dd) continue;
-            const f32x4 y = none ? f32x4{0, 0, 0, 0} : v[nt][x] * inv;
-            if (ES == 2)
-                *reinterpret_cast<uint2 *>(a.out + at[nt].o + dim(x) * 2) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            else
-                *reinterpret_cast<f32x4 *>(a.out + at[nt].o + dim(x) * 4) = y;
-        }
+    for (int x = 0; x < OUT; ++x) {
+        if (dim(x) >= Dd) continue;
+        const f32x4 y = none ? f32x4{0, 0, 0, 0} : v[x] * inv;
+        if (ES == 2)
+            *reinterpret_cast<uint2 *>(a.out + at.o + dim(x) * 2) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+        else
+            *reinterpret_cast<f32x4 *>(a.out + at.o + dim(x) * 4) = y;
     }
 }
 

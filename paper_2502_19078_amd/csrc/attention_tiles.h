@@ -30,21 +30,21 @@ __device__ __forceinline__ void unrolled_(F &&f, std::integer_sequence<int, I...
 template <int N, class F>
 __device__ __forceinline__ void unrolled(F &&f) { unrolled_(f, std::make_integer_sequence<int, N>{}); }
 
-template <int DP>
+template <int ES, int DP>
 struct TilesShape {
-    static constexpr int KT = DP <= 128 ? 64 : 32;           // keys of a tile
-    static constexpr int KP = DP * 2 + 16, VP = DP * 2 + 32; // row pitches: K rows 4 banks apart, V rows 8
+    static constexpr int KT = ES == 2 && DP <= 128 ? 64 : 32;        // keys of a tile
+    static constexpr int KP = DP * ES + 16, VP = DP * ES + (ES == 2 ? 32 : 16);      // row pitches: K rows 4 banks apart, bf16 V rows 8
     static constexpr int BUF = KT * (KP + VP), LDS = 2 * BUF;
 };
 
-template <int DP, bool FULL>
+template <int ES, int DP, bool FULL>
 __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, const int id, char *lds)
 {
-    using S = TilesShape<DP>;
+    using S = TilesShape<ES, DP>;
     constexpr int KT = S::KT, KB = KT / 32, KP = S::KP, VP = S::VP, BUF = S::BUF;
-    constexpr int KD = DP / 16, DB = DP / 32;
-    constexpr int CPR = DP == 96 ? 16 : DP / 8, ROWS = KT * CPR / 256;      // threads a row, 16 bytes each; rows of K (and of V) a thread stages
-    constexpr bool WHOLE = FULL && CPR * 8 == DP;            // every thread has a chunk of the row
+    constexpr int KD = DP * ES / 32, DB = DP / 32;           // 32-byte chunks of a row, 16 bytes a lane; tiles of 32 output dimensions
+    constexpr int CPR = DP == 96 ? 128 / (16 / ES) : DP * ES / 16, ROWS = KT * CPR / 256;    // threads a row, 16 bytes each; rows of K (and of V) a thread stages
+    constexpr bool WHOLE = FULL && CPR * 16 == DP * ES;      // every thread has a chunk of the row
     static_assert(KT * CPR % 256 == 0 && 256 % CPR == 0, "whole passes");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -85,13 +85,13 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     const int wave_b = pre ? a.pre_n : min(wr1 / a.G, qlen - 1) + first_pos;
     const bool ragged = !pre && wr1 / a.G >= qlen;           // rows of padding among them
 
-    const unsigned int flip = a.scale2 < 0.0f ? 0x80008000u : 0u;      // a negative scale is the queries' sign
+    const unsigned int flip = a.scale2 < 0.0f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;      // a negative scale is the queries' sign
     const float scale2 = fmaxf(fabsf(a.scale2), 1e-37f);     // (positive, so that -inf stays what it is)
     u32x4 qf[KD];
 #pragma unroll
     for (int c = 0; c < KD; ++c) {
         const int off = 32 * c + 16 * hh;
-        const bool in = FULL || off < Dd * 2;
+        const bool in = FULL || off < Dd * ES;
         qf[c] = *reinterpret_cast<const u32x4 *>(a.q + row_at(a, pre, b, h, rc, rc / a.G).q + (in ? off : 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) qf[c][e] = in ? qf[c][e] ^ flip : 0u;
@@ -99,7 +99,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 
     const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
     const int first_key = tid / CPR, col = tid % CPR * 16;   // of the chunks that this thread stages: keys first_key + j * (256 / CPR)
-    const bool in = WHOLE || col < Dd * 2;
+    const bool in = WHOLE || col < Dd * ES;
     const unsigned int lane_off = (unsigned int)first_key * (unsigned int)kv.sn + (in ? col : 0), step_off = 256 / CPR * (unsigned int)kv.sn;
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
     auto fetch = [&](int i) {
@@ -132,7 +132,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     };
     const unsigned int put_k = first_key * KP + col, put_v = KT * KP + first_key * VP + col;
     auto put = [&](int buf) {
-        if (CPR * 8 != DP && col >= DP * 2) return;
+        if (CPR * 16 != DP * ES && col >= DP * ES) return;
         char *to_k = lds + (put_k + buf * BUF), *to_v = lds + (put_v + buf * BUF);
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
@@ -163,16 +163,24 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 #pragma unroll
             for (int k = 0; k < KB; ++k) {
                 const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
-                s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
-            }
-        // six fragments ahead of the products
-        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+                if constexpr (ES == 2)
+                    s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
+                else
 #pragma unroll
-        for (int x = 0; x < KD * KB - 6; ++x) {
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned int ka = kf[e], qb = qf[c][e];
+                        s[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka), __uint_as_float(qb), c || e ? s[k] : zero, 0, 0, 0);
+                    }
+            }
+        if constexpr (ES == 2) {                             // six fragments ahead of the products
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int x = 0; x < KD * KB - 6; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (EDGE) {
             if (!all) {
@@ -198,42 +206,57 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             }
         }
         const float base = EDGE && m == NEG_INF ? 0.0f : m;
-        // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and the
-        // reads of V four products ahead.
-        constexpr int STEPS = 2 * KB, AHEAD = 4;
-        u32x4 vt[AHEAD], pk[2];
-        auto weight = [&](auto step, int e) {                // the e-th of the step's eight weights of this lane
-            constexpr int st = decltype(step)::value, k = st / 2, c = st % 2;
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[k][8 * c + e], scale2, -base));
-            l += p;
-            s[k][8 * c + e] = p;
-            if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
-        };
-        const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
-        auto read_v = [&](int x) {
-            const char *from = src + x / DB * 16 * VP + x % DB * 64;
-            const uint2 u0 = read_tr16(from), u1 = read_tr16(from + 8 * VP);
-            vt[x % AHEAD] = u32x4{u0.x, u0.y, u1.x, u1.y};
-        };
+        if constexpr (ES == 2) {
+            // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and the
+            // reads of V four products ahead.
+            constexpr int STEPS = 2 * KB, AHEAD = 4;
+            u32x4 vt[AHEAD], pk[2];
+            auto weight = [&](auto step, int e) {                // the e-th of the step's eight weights of this lane
+                constexpr int st = decltype(step)::value, k = st / 2, c = st % 2;
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[k][8 * c + e], scale2, -base));
+                l += p;
+                s[k][8 * c + e] = p;
+                if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
+            };
+            const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
+            auto read_v = [&](int x) {
+                const char *from = src + x / DB * 16 * VP + x % DB * 64;
+                const uint2 u0 = read_tr16(from), u1 = read_tr16(from + 8 * VP);
+                vt[x % AHEAD] = u32x4{u0.x, u0.y, u1.x, u1.y};
+            };
 #pragma unroll
-        for (int x = 0; x < AHEAD; ++x) read_v(x);
+            for (int x = 0; x < AHEAD; ++x) read_v(x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) weight(std::integral_constant<int, 0>{}, e);
-        unrolled<STEPS>([&](auto step) {
-            constexpr int st = decltype(step)::value;
+            for (int e = 0; e < 8; ++e) weight(std::integral_constant<int, 0>{}, e);
+            unrolled<STEPS>([&](auto step) {
+                constexpr int st = decltype(step)::value;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                __builtin_amdgcn_sched_barrier(0);
-                const int x = st * DB + d;
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, pk[st & 1]), o[d], 0, 0, 0);
-                if (x + AHEAD < STEPS * DB) read_v(x + AHEAD);
-                if constexpr (st + 1 < STEPS) {
+                for (int d = 0; d < DB; ++d) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int x = st * DB + d;
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, pk[st & 1]), o[d], 0, 0, 0);
+                    if (x + AHEAD < STEPS * DB) read_v(x + AHEAD);
+                    if constexpr (st + 1 < STEPS) {
 #pragma unroll
-                    for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) weight(std::integral_constant<int, st + 1>{}, e);
+                        for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) weight(std::integral_constant<int, st + 1>{}, e);
+                    }
                 }
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[0][e] = __builtin_amdgcn_exp2f(fmaf(s[0][e], scale2, -base));
+                l += s[0][e];
             }
-        });
-        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {                   // keys 8 (e / 4) + 4 hh + e % 4
+                const char *src = vb + (8 * (e >> 2) + 4 * hh + (e & 3)) * VP + n32 * 4;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float *>(src + d * 128), s[0][e], o[d], 0, 0, 0);
+            }
+        }
         steady = !__any(l > 0x1p60f || (EDGE && m == NEG_INF));
     };
 
@@ -283,7 +306,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     for (unsigned int left = again; left; left &= left - 1) {
         const int t = __builtin_ctz(left);
         const RowAt at = row_at(a, pre, b, h, r0 + wave * 32 + t, (r0 + wave * 32 + t) / a.G);
-        attn_store_again<2>(a, attn_row_again<2>(a, kr, kv, kp, vp, a.q + at.q, __shfl(row_pos, t), k0, k1), at, split);
+        attn_store_again<ES>(a, attn_row_again<ES>(a, kr, kv, kp, vp, a.q + at.q, __shfl(row_pos, t), k0, k1), at, split);
     }
     if (r >= rows || (again >> n32 & 1)) return;
     const RowAt to_row = row_at(a, pre, b, h, r, r / a.G);
@@ -311,8 +334,12 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
         for (int e = 0; e < 16; e += 4) {
             const int dim = 32 * d + 2 * e + 4 * hh;
             if (!FULL && dim >= Dd) continue;
-            const uint2 v = make_uint2(pack_bf16(o[d][e] * inv, o[d][e + 1] * inv), pack_bf16(o[d][e + 2] * inv, o[d][e + 3] * inv));
-            *reinterpret_cast<uint2 *>(a.out + to_row.o + dim * 2) = nothing ? make_uint2(0, 0) : v;
+            f32x4 y = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]} * inv;
+            if (nothing) y = f32x4{0, 0, 0, 0};
+            if (ES == 2)
+                *reinterpret_cast<uint2 *>(a.out + to_row.o + dim * 2) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            else
+                *reinterpret_cast<f32x4 *>(a.out + to_row.o + dim * 4) = y;
         }
 }
 
