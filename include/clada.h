@@ -429,6 +429,7 @@ clada_status clada_static_ffn_decode(clada_ctx *ctx, const clada_layer *layer, c
 #define CLADA_ATTN_MAX_HEADS 1024  /* query heads                             */
 #define CLADA_ATTN_MAX_BATCH 4096  /* sequences of a call                     */
 #define CLADA_ATTN_MAX_ROWS (1 << 20) /* B * T of a call                      */
+#define CLADA_ATTN_MAX_CAPACITY (1 << 30) /* rows of a cache                  */
 
 typedef struct {
     void *data;
@@ -499,7 +500,8 @@ size_t clada_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t d);
  * Query head h reads key head h / (Hq / heads).  A query that sees nothing (a row past q_lens[b], a negative position) gives zeros
  * and an lse of -inf.  T = 1 is a decode step, T = lens a prompt.  Without a ring lens[b] <= capacity (more is taken as capacity);
  * with one, window >= 1, ring >= window + T - 1 and sinks <= n_sink.  Cache rows that a query does not see do not reach its output,
- * whatever they hold.  Scores, sums and outputs are accumulated in fp32.  Bit-reproducible from run to run. */
+ * whatever they hold.  out must not overlap q.  Scores, sums and outputs are accumulated in fp32; the weights of bf16 calls enter the product
+ * with v as one bf16 (T > 1 and more than 16 rows T Hq / heads) or as two.  Bit-reproducible from run to run. */
 clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada_kv_cache *cache, const int32_t *lens,
                                const int32_t *q_lens, int32_t B, int32_t T, int32_t Hq, int32_t window, int32_t sinks, float scale,
                                const clada_heads *out, float *lse, void *hip_stream);

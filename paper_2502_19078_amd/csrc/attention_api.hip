@@ -9,7 +9,7 @@ clada_status clada_check_kv(clada_ctx *ctx, const clada_kv_cache *c, const char 
     if (c->dtype != CLADA_F32 && c->dtype != CLADA_BF16) return clada_fail(ctx, CLADA_ERR_DTYPE, "%s: unknown dtype %d", what, (int)c->dtype);
     if (c->d < 8 || c->d > CLADA_ATTN_MAX_D || c->d % 8)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: heads of %d values, not a multiple of 8 in [8,%d]", what, c->d, CLADA_ATTN_MAX_D);
-    if (c->batch < 1 || c->heads < 1 || c->heads > CLADA_ATTN_MAX_HEADS || c->capacity < 1)
+    if (c->batch < 1 || c->heads < 1 || c->heads > CLADA_ATTN_MAX_HEADS || c->capacity < 1 || c->capacity > CLADA_ATTN_MAX_CAPACITY)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: %d sequences, %d heads, %d rows", what, c->batch, c->heads, c->capacity);
     if (c->n_sink < 0 || c->ring < 0 || (c->ring && (int64_t)c->n_sink + c->ring > c->capacity))
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: n_sink=%d and a ring of %d rows in a capacity of %d", what, c->n_sink, c->ring, c->capacity);
@@ -35,7 +35,7 @@ clada_status clada_check_heads(clada_ctx *ctx, const clada_heads *h, int32_t dty
 namespace {
 
 constexpr int MAX_SPLITS = 256;                              // of one row's keys
-constexpr int64_t PART_ROWS = 65536;                         // rows whose splits a call keeps partial results of, more or less
+constexpr int MAX_CU = 256;                                  // of the device that the workspace bound is made for
 
 size_t part_bytes(int64_t parts, int d) { return align_up((size_t)parts * 8, 256) + (size_t)parts * d * 4; }
 
@@ -45,12 +45,14 @@ AttnKV kv_of(const clada_kv_cache *c)
     return {(const char *)c->k, (const char *)c->v, c->stride_b * es, c->stride_h * es, c->stride_n * es, c->capacity, c->n_sink, c->ring};
 }
 
-// Splits of `keys` keys for `units` tiles, so that the launch fills the chip: two workgroups a compute unit, no split under 128 keys (one step of its
-// waves).  513 keys of one key head of 256 values: four splits and the launch that joins them 15 us, one workgroup 26 us (a compute unit
-// loads 26 bytes a clock).
-int splits_for(int64_t units, int64_t keys, int num_cu)
+// Splits of `keys` keys for `units` tiles, so that the launch has about `wgs` workgroups; no split under 128 keys (one step of the few-row kernel's
+// waves; two tiles).  Few rows: one workgroup a compute unit streams as fast as two (8 windows of 4096: 33.5 against 34.7 us), with half
+// the partial results; tiles take two (64 queries a sequence: 24.3 and 22.7 us).  A shared prefix and the sequences' own keys take one a
+// compute unit each (16 sequences behind 8192 rows 20.2 us, twice as many 27.2; 48 behind 4095: 38.2 and 44).  One workgroup for all keys
+// of a short sequence costs more than the launch that joins splits (513 keys of 256 values: 26 us against 15).
+int splits_for(int64_t units, int64_t keys, int64_t wgs)
 {
-    const int64_t want = (2 * (int64_t)num_cu + units - 1) / units, most = (keys + 127) / 128;
+    const int64_t want = (wgs + units - 1) / units, most = (keys + 127) / 128;
     int64_t s = want < most ? want : most;
     if (s > MAX_SPLITS) s = MAX_SPLITS;
     return s < 1 ? 1 : (int)s;
@@ -112,8 +114,18 @@ extern "C" {
 size_t clada_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t d)
 {
     if (B < 1 || T < 1 || Hq < 1 || d < 1) return 256;
-    const int64_t rows = (int64_t)B * T * Hq, most = rows * 2 * MAX_SPLITS, cap = 2 * (PART_ROWS + 2 * rows);
-    return part_bytes(most < cap ? most : cap, d) + 256;
+    // Partial results, one a row and split, of the largest call up to these sizes.  Tiles of 128 rows are split where there are fewer than 2 MAX_CU,
+    // into 2 MAX_CU / tiles + 1 at most; tiles of 16, and a prefix's of 128, where there are fewer than MAX_CU, into MAX_CU / tiles + 1.  (A single
+    // token may need the last two together.)
+    const int64_t one = (int64_t)B * Hq, rows = one * T, wide = 128 * 2 * MAX_CU;
+    int64_t parts = (16 + 128) * MAX_CU + 2 * one;
+    if (parts > one * 2 * MAX_SPLITS) parts = one * 2 * MAX_SPLITS;
+    if (T > 1) {
+        int64_t many = wide + (rows < wide ? rows : wide);
+        if (many > rows * MAX_SPLITS) many = rows * MAX_SPLITS;
+        if (many > parts) parts = many;
+    }
+    return part_bytes(parts, d) + 256;
 }
 
 clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada_kv_cache *cache, const int32_t *lens, const int32_t *q_lens,
@@ -136,20 +148,19 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     AttnArgs a = {};
     fill(a, q, out, cache, lens, B, T, Hq, scale, lse);
     a.q_lens = q_lens;
-    a.window = window;
-    a.sinks = window ? sinks : 0;
+    a.window = cache->ring == 0 && window >= cache->capacity ? 0 : window;       // (as wide as the cache: everything)
+    a.sinks = a.window ? (sinks < cache->capacity ? sinks : cache->capacity) : 0;
     const int es = (int)dtype_size(cache->dtype);
     const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
     const int tile = path == ATTN_ROWS ? 16 : 128;
     a.own_tiles = (T * a.G + tile - 1) / tile;
     const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
     int64_t keys = cache->capacity;                          // what a tile can see at most
-    if (window) {
-        const int64_t seen = (int64_t)window + sinks + tile / a.G;
+    if (a.window) {
+        const int64_t seen = (int64_t)a.window + a.sinks + tile / a.G;
         if (seen < keys) keys = seen;
     }
-    a.splits = splits_for(units, keys, ctx->num_cu);
-    if (units * a.splits > INT32_MAX) return clada_fail(ctx, CLADA_ERR_SHAPE, "the call has too many rows");
+    a.splits = splits_for(units, keys, path == ATTN_ROWS ? ctx->num_cu : 2 * ctx->num_cu);
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
     return CLADA_OK;

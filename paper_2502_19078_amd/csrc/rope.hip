@@ -361,6 +361,7 @@ extern "C" clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, co
     int per = 8;
     while (per > 1 && (int64_t)a.tokens * ((heads + per - 1) / per) * lg < (int64_t)ctx->num_cu * 1024) per /= 2;
     a.slabs = (heads + per - 1) / per;
+    if ((int64_t)a.tokens * a.slabs * lg > (INT64_C(1) << 31)) return clada_fail(ctx, CLADA_ERR_SHAPE, "the call has too many heads and tokens");
     const bool pairs = rope->layout == CLADA_ROPE_PAIRS;
     hipStream_t s = (hipStream_t)hip_stream;
     if (es == 2) {
