@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_attn_tiles(const AttnArgs a)
 {
     __shared__ __align__(16) char lds[TilesShape<ES, DP>::LDS];
-    attn_tiles<ES, DP, FULL>(a, false, blockIdx.x, lds);
+    attn_tiles<ES, DP, FULL, false>(a, false, blockIdx.x, lds);
 }
 
 // A shared prefix for more than 16 rows: its workgroups first, then those of the sequences' own keys, in one launch.
@@ -32,7 +32,7 @@ k_attn_prefix(const AttnArgs a)
     constexpr int L0 = TilesShape<ES, DP>::LDS, L1 = RowsShape<ES, DP>::LDS;
     __shared__ __align__(16) char lds[L0 > L1 ? L0 : L1];
     const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
-    if (id < pre_blocks) attn_tiles<ES, DP, FULL>(a, true, id, lds);
+    if (id < pre_blocks) attn_tiles<ES, DP, FULL, ES == 2>(a, true, id, lds);
     else attn_rows<ES, DP, FULL>(a, false, id - pre_blocks, lds);
 }
 
@@ -50,6 +50,11 @@ k_attn_join(const AttnArgs a)
     const int gr = tid / TPR, dim = tid % TPR * 4;
     float l = 0.0f, top = NEG_INF;
     f32x4 o = {0, 0, 0, 0};
+    const float *po = a.part_o + row * splits * a.D + dim;
+    f32x4 first[4];                                          // on their way while the factors are formed
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (gr + j * GR < splits && dim < a.D) first[j] = *reinterpret_cast<const f32x4 *>(po + (int64_t)(gr + j * GR) * a.D);
     for (int s0 = 0; s0 < splits; s0 += 256) {               // (512 splits at most: two rounds)
         const float2 v = s0 + tid < splits ? a.part_ml[row * splits + s0 + tid] : make_float2(NEG_INF, 0.0f);
         const float most = wave_max(v.x);
@@ -57,7 +62,7 @@ k_attn_join(const AttnArgs a)
         if (lane == 0) s_red[wave] = most;
         __syncthreads();
         const float mn = fmaxf(top, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
-        // a split without keys has written no values: none are read for it
+        // a split without keys has written no values: none are used for it
         const float f = v.x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(v.x - mn), g = top == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(top - mn);
         s_f[tid] = v.y == 0.0f ? -1.0f : f;
         const float sum = wave_sum(v.x == NEG_INF ? v.y : v.y * f);
@@ -67,10 +72,17 @@ k_attn_join(const AttnArgs a)
         o *= g;
         top = mn;
         const int n = min(splits - s0, 256);
+        if (dim >= a.D) continue;
+        int s = gr;
+        if (s0 == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j, s += GR)
+                if (s < n && s_f[s] != -1.0f) o += first[j] * s_f[s];
+        }
 #pragma unroll 4
-        for (int s = gr; s < n; s += GR) {
+        for (; s < n; s += GR) {
             const float fs = s_f[s];
-            if (fs != -1.0f && dim < a.D) o += *reinterpret_cast<const f32x4 *>(a.part_o + (row * splits + s0 + s) * a.D + dim) * fs;
+            if (fs != -1.0f) o += *reinterpret_cast<const f32x4 *>(po + (int64_t)(s0 + s) * a.D) * fs;
         }
     }
     s_o[gr][tid % TPR] = o;

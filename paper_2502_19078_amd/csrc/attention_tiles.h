@@ -37,7 +37,8 @@ struct TilesShape {
     static constexpr int BUF = KT * (KP + VP), LDS = 2 * BUF;
 };
 
-template <int ES, int DP, bool FULL>
+// FINE: the weights of a bf16 call enter the second product as two bf16, 16 bits, in two products.
+template <int ES, int DP, bool FULL, bool FINE>
 __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, const int id, char *lds)
 {
     using S = TilesShape<ES, DP>;
@@ -102,17 +103,24 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     const bool in = WHOLE || col < Dd * ES;
     const unsigned int lane_off = (unsigned int)first_key * (unsigned int)kv.sn + (in ? col : 0), step_off = 256 / CPR * (unsigned int)kv.sn;
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
+    // A whole tile of consecutive cache rows has one base for all lanes (offsets in 32 bits: no row further than 32 MiB from the next).
+    auto regular = [&](int i) { return i + KT <= k1 && kv.sn < (1 << 25) && kr.row(kr.pos(i + KT - 1), kv) - kr.row(kr.pos(i), kv) == KT - 1; };
+    __amdgpu_buffer_rsrc_t k_tile, v_tile;
+    auto aim = [&](int i) {                                  // at a regular tile
+        const int64_t at = kr.row(kr.pos(i), kv) * kv.sn;
+        k_tile = __builtin_amdgcn_make_buffer_rsrc((void *)(kp + at), 0, -1, 0x00027000);
+        v_tile = __builtin_amdgcn_make_buffer_rsrc((void *)(vp + at), 0, -1, 0x00027000);
+    };
+    auto take = [&](int q) {                                 // transfer q of 2 ROWS of that tile: K, V, K, ..
+        const int j = q / 2;
+        if (q & 1) sv[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(v_tile, lane_off, j * step_off, 0));
+        else sk[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k_tile, lane_off, j * step_off, 0));
+    };
     auto fetch = [&](int i) {
-        // A whole tile of consecutive cache rows has one base for all lanes (offsets in 32 bits: no row further than 32 MiB from the next)
-        const int64_t row0 = kr.row(kr.pos(i), kv);
-        if (i + KT <= k1 && kv.sn < (1 << 25) && kr.row(kr.pos(i + KT - 1), kv) - row0 == KT - 1) {
-            const __amdgpu_buffer_rsrc_t kt = __builtin_amdgcn_make_buffer_rsrc((void *)(kp + row0 * kv.sn), 0, -1, 0x00027000);
-            const __amdgpu_buffer_rsrc_t vt = __builtin_amdgcn_make_buffer_rsrc((void *)(vp + row0 * kv.sn), 0, -1, 0x00027000);
+        if (regular(i)) {
+            aim(i);
 #pragma unroll
-            for (int j = 0; j < ROWS; ++j) {
-                sk[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kt, lane_off, j * step_off, 0));
-                sv[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, lane_off, j * step_off, 0));
-            }
+            for (int q = 0; q < 2 * ROWS; ++q) take(q);
         } else {
             int key0 = i + first_key;
             asm volatile("" : "+v"(key0));                   // (nothing of this is kept in registers across the loop)
@@ -125,20 +133,19 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                 if (key >= k1) sv[j] = u32x4{0, 0, 0, 0};
             }
         }
-        if (!WHOLE && !in) {
-#pragma unroll
-            for (int j = 0; j < ROWS; ++j) sk[j] = sv[j] = u32x4{0, 0, 0, 0};
-        }
     };
-    const unsigned int put_k = first_key * KP + col, put_v = KT * KP + first_key * VP + col;
+    // (threads without a chunk write into the row's padding)
+    const unsigned int put_k = first_key * KP + min(col, DP * ES), put_v = KT * KP + first_key * VP + min(col, DP * ES);
+    auto put_one = [&](int buf, int q) {                     // transfer q into LDS
+        const int j = q / 2;
+        u32x4 x = q & 1 ? sv[j] : sk[j];
+        if (!WHOLE && !in) x = u32x4{0, 0, 0, 0};
+        char *to = lds + ((q & 1 ? put_v : put_k) + buf * BUF) + j * (256 / CPR) * (q & 1 ? VP : KP);
+        *reinterpret_cast<u32x4 *>(to) = x;
+    };
     auto put = [&](int buf) {
-        if (CPR * 16 != DP * ES && col >= DP * ES) return;
-        char *to_k = lds + (put_k + buf * BUF), *to_v = lds + (put_v + buf * BUF);
 #pragma unroll
-        for (int j = 0; j < ROWS; ++j) {
-            *reinterpret_cast<u32x4 *>(to_k + j * (256 / CPR) * KP) = sk[j];
-            *reinterpret_cast<u32x4 *>(to_v + j * (256 / CPR) * VP) = sv[j];
-        }
+        for (int q = 0; q < 2 * ROWS; ++q) put_one(buf, q);
     };
 
     // A row's maximum is that of the first tile that it sees; its weights grow past 1 from there on (as floats they lose nothing) and are
@@ -152,10 +159,21 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
     bool steady = false;                                     // every row has its maximum, and no sum has passed 2^60
-    // One tile for this wave's rows.  EDGE: some of them do not see all of it, or a maximum has to be set or moved.
-    auto multiply = [&](auto edge, int i, const char *kb, bool all) {
+    // One tile for this wave's rows.  EDGE: some of them do not see all of it, or a maximum has to be set or moved.  Otherwise the next tile goes
+    // into LDS, and the one after it (regular, aimed at) is taken, transfer by transfer between the products: the loads of all waves pass one
+    // address unit, and in one place they would hold up the waves for 800 clocks of a tile.
+    auto multiply = [&](auto edge, int i, int buf, bool all) {
         constexpr bool EDGE = decltype(edge)::value;
-        const char *vb = kb + KT * KP;
+        const char *kb = lds + buf * BUF, *vb = kb + KT * KP;
+        auto stage = [&](int x, int of) {                    // behind product x of `of`
+            if constexpr (!EDGE) {
+#pragma unroll
+                for (int q = 2 * ROWS * x / of; q < 2 * ROWS * (x + 1) / of; ++q) {
+                    put_one(buf ^ 1, q);
+                    take(q);
+                }
+            }
+        };
         f32x16 s[KB];
         const f32x16 zero = {};
 #pragma unroll
@@ -210,13 +228,18 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and the
             // reads of V four products ahead.
             constexpr int STEPS = 2 * KB, AHEAD = 4;
-            u32x4 vt[AHEAD], pk[2];
+            u32x4 vt[AHEAD], pk[2], lo[FINE ? 2 : 1];
             auto weight = [&](auto step, int e) {                // the e-th of the step's eight weights of this lane
                 constexpr int st = decltype(step)::value, k = st / 2, c = st % 2;
                 const float p = __builtin_amdgcn_exp2f(fmaf(s[k][8 * c + e], scale2, -base));
                 l += p;
                 s[k][8 * c + e] = p;
-                if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
+                if (e & 1) {
+                    const float p0 = s[k][8 * c + e - 1];
+                    const unsigned int u = pack_bf16(p0, p);
+                    pk[st & 1][e >> 1] = u;
+                    if (FINE) lo[FINE ? st & 1 : 0][e >> 1] = pack_bf16(p0 - __uint_as_float(u << 16), p - __uint_as_float(u & 0xffff0000u));
+                }
             };
             const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
             auto read_v = [&](int x) {
@@ -235,7 +258,10 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
                     __builtin_amdgcn_sched_barrier(0);
                     const int x = st * DB + d;
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, pk[st & 1]), o[d], 0, 0, 0);
+                    if constexpr (FINE)
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vt[x % AHEAD]), __builtin_bit_cast(bf16x8, lo[st & 1]), o[d], 0, 0, 0);
                     if (x + AHEAD < STEPS * DB) read_v(x + AHEAD);
+                    stage(x, STEPS * DB);
                     if constexpr (st + 1 < STEPS) {
 #pragma unroll
                         for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) weight(std::integral_constant<int, st + 1>{}, e);
@@ -255,6 +281,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float *>(src + d * 128), s[0][e], o[d], 0, 0, 0);
+                stage(e, 16);
             }
         }
         steady = !__any(l > 0x1p60f || (EDGE && m == NEG_INF));
@@ -274,11 +301,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
         none = idle || p_first > wave_b || (a.window && p_first >= a.sinks && p_last <= wave_a - a.window && wave_a >= 0);
         all = last == i + KT - 1 && !ragged && (pre || (p_last <= wave_a && (a.window == 0 || p_first > wave_b - a.window || p_last < a.sinks)));
     };
-    auto next = [&]() {                                      // the next tile into LDS, the one after it on its way
-        if (i + KT < k1) {
-            put(buf ^ 1);
-            if (i + 2 * KT < k1) fetch(i + 2 * KT);
-        }
+    auto step = [&]() {
         tile_barrier();
         buf ^= 1;
         i += KT;
@@ -286,12 +309,17 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     // The waves of a workgroup may be in different loops; every tile is one barrier in both.
     while (i < k1) {
         look();
-        if (!none) multiply(std::true_type{}, i, lds + buf * BUF, all);
-        next();
-        for (; i < k1; next()) {
+        if (!none) multiply(std::true_type{}, i, buf, all);
+        if (i + KT < k1) {
+            put(buf ^ 1);
+            if (i + 2 * KT < k1) fetch(i + 2 * KT);
+        }
+        step();
+        for (; i < k1; step()) {
             look();
-            if (none || !all || !steady) break;
-            multiply(std::false_type{}, i, lds + buf * BUF, true);
+            if (none || !all || !steady || !regular(i + 2 * KT)) break;
+            aim(i + 2 * KT);
+            multiply(std::false_type{}, i, buf, true);
         }
     }
     l += __shfl_xor(l, 32);
