@@ -8,10 +8,10 @@
 namespace {
 
 template <int ES, int DP, bool FULL>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(256, ES == 2 || DP <= 128 ? 2 : 1)
 k_attn_rows(const AttnArgs a)
 {
-    __shared__ __align__(16) char lds[RowsShape<ES, DP>::LDS];
+    __shared__ __align__(16) char lds[RowsShape<ES, DP, FULL>::LDS];
     const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
     attn_rows<ES, DP, FULL>(a, id < pre_blocks, id < pre_blocks ? id : id - pre_blocks, lds);
 }
@@ -29,7 +29,7 @@ template <int ES, int DP, bool FULL>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_attn_prefix(const AttnArgs a)
 {
-    constexpr int L0 = TilesShape<ES, DP>::LDS, L1 = RowsShape<ES, DP>::LDS;
+    constexpr int L0 = TilesShape<ES, DP>::LDS, L1 = RowsShape<ES, DP, FULL>::LDS;
     __shared__ __align__(16) char lds[L0 > L1 ? L0 : L1];
     const int pre_blocks = a.Hkv * a.pre_tiles * a.pre_splits, id = blockIdx.x;
     if (id < pre_blocks) attn_tiles<ES, DP, FULL, ES == 2>(a, true, id, lds);

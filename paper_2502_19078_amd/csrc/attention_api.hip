@@ -46,10 +46,8 @@ AttnKV kv_of(const clada_kv_cache *c)
 }
 
 // Splits of `keys` keys for `units` tiles, so that the launch has about `wgs` workgroups; no split under 128 keys (one step of the few-row kernel's
-// waves; two tiles).  Few rows: one workgroup a compute unit streams as fast as two (8 windows of 4096: 33.5 against 34.7 us), with half
-// the partial results; tiles take two (64 queries a sequence: 24.3 and 22.7 us).  A shared prefix and the sequences' own keys take one a
-// compute unit each (16 sequences behind 8192 rows 20.2 us, twice as many 27.2; 48 behind 4095: 38.2 and 44).  One workgroup for all keys
-// of a short sequence costs more than the launch that joins splits (513 keys of 256 values: 26 us against 15).
+// waves; two tiles).  One workgroup for all keys of a short sequence costs more than the launch that joins splits (513 keys of one
+// head of 256 values: 26 us against 15).
 int splits_for(int64_t units, int64_t keys, int64_t wgs)
 {
     const int64_t want = (wgs + units - 1) / units, most = (keys + 127) / 128;
@@ -160,7 +158,9 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
         const int64_t seen = (int64_t)a.window + a.sinks + tile / a.G;
         if (seen < keys) keys = seen;
     }
-    a.splits = splits_for(units, keys, path == ATTN_ROWS ? ctx->num_cu : 2 * ctx->num_cu);
+    // Few rows: one workgroup a compute unit streams cache rows of 256 bytes and more as fast as two, with half the partial results (8 sequences of 8192
+    // rows, 8 key heads of 128 values: 54.8 against 57 us); narrower ones it does not (64 values: 37.8 against 33).  Tiles take two.
+    a.splits = splits_for(units, keys, path == ATTN_ROWS && cache->d * es >= 256 ? ctx->num_cu : 2 * ctx->num_cu);
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
     return CLADA_OK;
@@ -194,6 +194,8 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     const int tile = path == ATTN_ROWS ? 16 : 128;
     a.pre_tiles = (B * a.G + tile - 1) / tile;
     a.own_tiles = (a.G + 15) / 16;
+    // One workgroup a compute unit for the prefix and one for the sequences' own keys: 16 sequences behind 8192 rows 20.2 us, with two each 27.2
+    // (48 behind 4095: 38.2 and 44).
     a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
     a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
     if ((st = place_parts(ctx, a)) != CLADA_OK) return st;

@@ -4,7 +4,7 @@
 // One pass over the keys with a running maximum and sum per row, in base 2.
 //
 // Bound by the cache's bytes (HBM): a key head's rows of the cache are read once for all query heads of its group.  A workgroup takes a tile
-// of 16 rows and one split of their keys; its four waves take 32 (fp32: 16) keys in turn, each with a running softmax of its own, so
+// of 16 rows and one split of their keys; its four waves take 32 or 16 keys in turn, each with a running softmax of its own, so
 // nothing waits inside the loop; the waves' results are joined through LDS, those of the splits by k_attn_join.
 //
 // Scores are formed transposed, S^T = K Q^T: a lane then holds scores of one row only, keys 4 (lane / 16) + i of each 16, and the same
@@ -17,18 +17,20 @@
 namespace {
 
 // ES: bytes a value.  DP: D rounded up to the products' tiles; FULL: D == DP.
-template <int ES, int DP>
+// Keys of a step of a wave.  bf16: 32; 16 for 256 values (registers for one wave a SIMD otherwise: 8 sequences of 8192 rows, 8 key heads, 177 us
+// with 32 keys, 98 with 16) and whole heads of 96 (52 and 44 us; 80 values in the same kernel 40 and 43).
+template <int ES, int DP, bool FULL>
 struct RowsShape {
-    static constexpr int KB = ES == 2 ? 2 : 1, KS = 16 * KB; // keys of a step
+    static constexpr int KB = ES == 4 || DP == 256 || (DP == 96 && FULL) ? 1 : 2, KS = 16 * KB;
     static constexpr int PITCH = DP * 2 + 32;                // V in LDS: rows 8 banks apart modulo 64
-    static constexpr int V_LDS = ES == 2 ? 4 * 32 * PITCH : 0, J_LDS = DP * 256 + 512 + 16;     // of the join: outputs and maxima of four waves
+    static constexpr int V_LDS = ES == 2 ? 4 * KS * PITCH : 0, J_LDS = DP * 256 + 512 + 16;     // of the join: outputs and maxima of four waves
     static constexpr int LDS = V_LDS > J_LDS ? V_LDS : J_LDS;
 };
 
 template <int ES, int DP, bool FULL>
 __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, const int block, char *lds)
 {
-    using S = RowsShape<ES, DP>;
+    using S = RowsShape<ES, DP, FULL>;
     constexpr int CH = DP * ES / 64;                         // chunks of 64 bytes in a row: lane group g holds 16 bytes of each
     constexpr int KB = S::KB, KS = S::KS, PITCH = S::PITCH;
     constexpr int DB = DP / 16;                              // tiles of 16 output dimensions
@@ -99,7 +101,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
     const int k0 = min(split * chunk, kr.n), k1 = min(k0 + chunk, kr.n);
 
     const char *kp = kv.k + b * kv.sb + h * kv.sh, *vp = kv.v + b * kv.sb + h * kv.sh;
-    char *my_v = lds + wave * 32 * PITCH;
+    char *my_v = lds + wave * KS * PITCH;
 
     f32x4 o[DB];
     float m = NEG_INF, l = 0.0f;
@@ -211,9 +213,9 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
             }
 
         if (ES == 2) {
-            u32x4 hi, lo;
+            u32x4 hi = {}, lo = {};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < 2 * KB; ++w) {
                 const float p0 = s[(w >> 1) % KB][2 * (w & 1)], p1 = s[(w >> 1) % KB][2 * (w & 1) + 1];
                 const unsigned int u = pack_bf16(p0, p1);
                 hi[w] = u;
@@ -222,6 +224,12 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const bool pre, con
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const char *src = my_v + (4 * g + (n16 >> 2)) * PITCH + d * 32 + (n16 & 3) * 8;
+                if constexpr (KB == 1) {
+                    const s16x4 vt = __builtin_bit_cast(s16x4, read_tr16(src));
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, make_uint2(hi[0], hi[1])), o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, make_uint2(lo[0], lo[1])), o[d], 0, 0, 0);
+                    continue;
+                }
                 const uint2 u0 = read_tr16(src), u1 = read_tr16(src + 16 * PITCH);
                 const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y});
                 o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, hi), o[d], 0, 0, 0);
