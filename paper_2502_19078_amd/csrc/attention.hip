@@ -24,7 +24,9 @@ k_attn_tiles(const AttnArgs a)
     attn_tiles<ES, DP, FULL, false>(a, false, blockIdx.x, lds);
 }
 
-// A shared prefix for more than 16 rows: its workgroups first, then those of the sequences' own keys, in one launch.
+// A shared prefix for more than 16 rows: its workgroups first, then those of the sequences' own keys, in one launch.  Bound by the bytes of both:
+// 16 sequences behind 8192 rows, 8 key heads of 128 values, 20 us (2.6 TB/s with the join); 48 behind 4095, 32 key heads, 38 (3.4).  Tiles
+// of 32 rows in attention_rows.h, which read the prefix once for every 32 rows, took 48 and 93.
 template <int ES, int DP, bool FULL>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_attn_prefix(const AttnArgs a)
@@ -38,6 +40,7 @@ k_attn_prefix(const AttnArgs a)
 
 // One workgroup a row: its splits' partial results joined in a fixed order.  TPR threads hold 4 values each of a row; the 256 / TPR groups take
 // splits in turn and are joined through LDS.  A split's factor is computed by one thread for all.
+// 4 us for 256 rows of four splits, 6 for 512 rows of 34: latency of a launch and two dependent loads.
 template <int ES, int TPR>
 __global__ void __launch_bounds__(256)
 k_attn_join(const AttnArgs a)

@@ -158,9 +158,9 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
         const int64_t seen = (int64_t)a.window + a.sinks + tile / a.G;
         if (seen < keys) keys = seen;
     }
-    // Few rows: one workgroup a compute unit streams cache rows of 256 bytes and more as fast as two, with half the partial results (8 sequences of 8192
+    // Few rows: one workgroup a compute unit streams heads of 128 values and more as fast as two, with half the partial results (8 sequences of 8192
     // rows, 8 key heads of 128 values: 54.8 against 57 us); narrower ones it does not (64 values: 37.8 against 33).  Tiles take two.
-    a.splits = splits_for(units, keys, path == ATTN_ROWS && cache->d * es >= 256 ? ctx->num_cu : 2 * ctx->num_cu);
+    a.splits = splits_for(units, keys, path == ATTN_ROWS && cache->d >= 128 ? ctx->num_cu : 2 * ctx->num_cu);
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
     return CLADA_OK;

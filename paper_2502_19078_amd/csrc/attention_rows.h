@@ -11,6 +11,10 @@
 // registers are the operand of O^T = V^T P^T when its keys are counted in that order.  K goes from memory into the operand registers as it
 // lies; bf16 V goes through LDS, where ds_read_tr16 turns it; fp32 V needs no turning.  The weights enter the second product as two bf16, 16
 // bits: the matrix cores have time to spare here.
+//
+// Measured, bf16, with the join of the splits (us): one token over 131071 rows of 8 key heads of 128 values 96 (5.6 TB/s); 8 tokens, each over a
+// window of 4096 and 4 sinks, 33 (4.1; 27 without the join's launch); 64 x 4096 rows of 32 key heads 705 (6.1); 513 rows of one head
+// of 256 values 14, of which a step of the loads is 2 and the chain of launches, lengths, first keys and join the rest.
 #pragma once
 #include "attention.h"
 
