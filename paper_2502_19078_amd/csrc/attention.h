@@ -32,7 +32,7 @@ struct AttnArgs {
 // Which kernel: tiles of 16 rows, of 128 rows, or a shared prefix in tiles of 128 rows with the sequences' own keys in tiles of 16.  Partial
 // results are joined where there are any.
 enum AttnPath { ATTN_ROWS, ATTN_TILES, ATTN_PREFIX };
-hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, hipStream_t stream);
+hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, int num_cu, hipStream_t stream);
 
 #ifdef __HIPCC__
 typedef __attribute__((ext_vector_type(4))) float f32x4;

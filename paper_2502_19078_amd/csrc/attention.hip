@@ -38,9 +38,29 @@ k_attn_prefix(const AttnArgs a)
     else attn_rows<ES, DP, FULL>(a, false, id - pre_blocks, lds);
 }
 
+// A joined row: four outputs of a thread, and the log of the sum by the thread that holds dim 0.
+template <int ES>
+__device__ __forceinline__ void join_store(const AttnArgs &a, const int64_t row, const int dim, f32x4 o, const float l, const float top)
+{
+    const int hq = (int)(row % a.Hq);
+    const int64_t bt = row / a.Hq;
+    const int b = a.T == 1 ? (int)bt : (int)(bt / a.T), t = (int)(bt - (int64_t)b * a.T);
+    int len, qlen;
+    sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
+    const bool none = a.pre_splits ? a.pre_n + len == 0 : t >= qlen || len - qlen + t < 0;
+    if (a.lse && dim == 0) a.lse[row] = none ? NEG_INF : top * 0.69314718055994531f + logf(l);
+    if (dim >= a.D) return;
+    o = none ? f32x4{0, 0, 0, 0} : o * (1.0f / l);
+    char *to = a.out + b * a.o_sb + t * a.o_st + hq * a.o_sh;
+    if (ES == 2)
+        *reinterpret_cast<uint2 *>(to + dim * 2) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+    else
+        *reinterpret_cast<f32x4 *>(to + dim * 4) = o;
+}
+
 // One workgroup a row: its splits' partial results joined in a fixed order.  TPR threads hold 4 values each of a row; the 256 / TPR groups take
 // splits in turn and are joined through LDS.  A split's factor is computed by one thread for all.
-// 4 us for 256 rows of four splits, 6 for 512 rows of 34: latency of a launch and two dependent loads.
+// 4 us for 256 rows of four splits, 5 for 512 rows of 34: latency of a launch and two dependent loads.
 template <int ES, int TPR>
 __global__ void __launch_bounds__(256)
 k_attn_join(const AttnArgs a)
@@ -93,20 +113,57 @@ k_attn_join(const AttnArgs a)
     if (gr) return;
 #pragma unroll
     for (int k = 1; k < GR; ++k) o += s_o[k][tid];
-    const int hq = (int)(row % a.Hq);
-    const int64_t bt = row / a.Hq;
-    const int b = a.T == 1 ? (int)bt : (int)(bt / a.T), t = (int)(bt - (int64_t)b * a.T);
-    int len, qlen;
-    sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
-    const bool none = a.pre_splits ? a.pre_n + len == 0 : t >= qlen || len - qlen + t < 0;
-    if (a.lse && tid == 0) a.lse[row] = none ? NEG_INF : top * 0.69314718055994531f + logf(l);
-    if (dim >= a.D) return;
-    o = none ? f32x4{0, 0, 0, 0} : o * (1.0f / l);
-    char *to = a.out + b * a.o_sb + t * a.o_st + hq * a.o_sh;
-    if (ES == 2)
-        *reinterpret_cast<uint2 *>(to + dim * 2) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+    join_store<ES>(a, row, dim, o, l, top);
+}
+
+// The same for at most FEW_SPLITS: TPR threads a row, 256 / TPR rows a workgroup, every thread forms the factors for itself; no LDS, no barriers.
+// Loads are not conditional, so that all are in flight together (with conditions 186 registers and slower than a workgroup a row up to 2112 rows).
+constexpr int FEW_SPLITS = 8;
+template <int ES, int TPR>
+__global__ void __launch_bounds__(256)
+k_attn_join_few(const AttnArgs a)
+{
+    const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    if (row >= (int64_t)a.B * a.T * a.Hq) return;
+    const int splits = a.splits + a.pre_splits, dim = threadIdx.x % TPR * 4;
+    const float *po = a.part_o + row * splits * a.D + (dim < a.D ? dim : 0);
+    float2 v[FEW_SPLITS];
+    f32x4 part[FEW_SPLITS];
+#pragma unroll
+    for (int s = 0; s < FEW_SPLITS; ++s) {
+        const int at = min(s, splits - 1);                   // (those past the last read it again and count for nothing)
+        v[s] = a.part_ml[row * splits + at];
+        part[s] = *reinterpret_cast<const f32x4 *>(po + at * a.D);
+    }
+#pragma unroll
+    for (int s = 0; s < FEW_SPLITS; ++s) {
+        if (s >= splits) v[s] = make_float2(NEG_INF, 0.0f);
+        if (v[s].y == 0.0f) part[s] = f32x4{0, 0, 0, 0};     // a split without keys has written no values
+    }
+    float l = 0.0f, top = NEG_INF;
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < FEW_SPLITS; ++s) top = fmaxf(top, v[s].x);
+#pragma unroll
+    for (int s = 0; s < FEW_SPLITS; ++s) {
+        const float f = v[s].x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(v[s].x - top);
+        l += v[s].x == NEG_INF ? v[s].y : v[s].y * f;
+        o += part[s] * f;
+    }
+    join_store<ES>(a, row, dim, o, l, top);
+}
+
+template <int ES, int TPR>
+void launch_join(const AttnArgs &a, int num_cu, hipStream_t stream)
+{
+    const int64_t rows = (int64_t)a.B * a.T * a.Hq;
+    constexpr int RW = 256 / TPR;
+    // Whole calls, us, a workgroup a row against this: 8 rows 14.3 / 14.9, 256 rows even, 1280 rows of 64 values 16.6 / 15.4, 4096 rows 22.0 / 17.6,
+    // 8192 rows of 128 values 43.0 / 36.2, 4096 rows of 256 values 55.7 / 53.1.
+    if (rows > 4 * num_cu && a.splits + a.pre_splits <= FEW_SPLITS)
+        hipLaunchKernelGGL((k_attn_join_few<ES, TPR>), dim3((unsigned int)((rows + RW - 1) / RW)), dim3(256), 0, stream, a);
     else
-        *reinterpret_cast<f32x4 *>(to + dim * 4) = o;
+        hipLaunchKernelGGL((k_attn_join<ES, TPR>), dim3((unsigned int)rows), dim3(256), 0, stream, a);
 }
 
 template <int ES, int DP, bool FULL>
@@ -137,22 +194,21 @@ void launch_type(const AttnArgs &a, AttnPath path, dim3 grid, hipStream_t stream
 
 }  // namespace
 
-hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, hipStream_t stream)
+hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, int num_cu, hipStream_t stream)
 {
     const dim3 grid((unsigned int)((int64_t)a.Hkv * a.pre_tiles * a.pre_splits + (int64_t)a.B * a.Hkv * a.own_tiles * a.splits));
     if (es == 2) launch_type<2>(a, path, grid, stream);
     else launch_type<4>(a, path, grid, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits + a.pre_splits == 1) return e;
-    const dim3 rows((unsigned int)((int64_t)a.B * a.T * a.Hq)), block(256);
     if (es == 2) {
-        if (a.D <= 64) hipLaunchKernelGGL((k_attn_join<2, 16>), rows, block, 0, stream, a);
-        else if (a.D <= 128) hipLaunchKernelGGL((k_attn_join<2, 32>), rows, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_attn_join<2, 64>), rows, block, 0, stream, a);
+        if (a.D <= 64) launch_join<2, 16>(a, num_cu, stream);
+        else if (a.D <= 128) launch_join<2, 32>(a, num_cu, stream);
+        else launch_join<2, 64>(a, num_cu, stream);
     } else {
-        if (a.D <= 64) hipLaunchKernelGGL((k_attn_join<4, 16>), rows, block, 0, stream, a);
-        else if (a.D <= 128) hipLaunchKernelGGL((k_attn_join<4, 32>), rows, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_attn_join<4, 64>), rows, block, 0, stream, a);
+        if (a.D <= 64) launch_join<4, 16>(a, num_cu, stream);
+        else if (a.D <= 128) launch_join<4, 32>(a, num_cu, stream);
+        else launch_join<4, 64>(a, num_cu, stream);
     }
     return hipGetLastError();
 }

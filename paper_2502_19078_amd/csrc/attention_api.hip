@@ -162,7 +162,7 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     // rows, 8 key heads of 128 values: 54.8 against 57 us); narrower ones it does not (64 values: 37.8 against 33).  Tiles take two.
     a.splits = splits_for(units, keys, path == ATTN_ROWS && cache->d >= 128 ? ctx->num_cu : 2 * ctx->num_cu);
     if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
-    CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
+    CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, ctx->num_cu, (hipStream_t)hip_stream));
     return CLADA_OK;
 }
 
@@ -199,7 +199,7 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
     a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
     if ((st = place_parts(ctx, a)) != CLADA_OK) return st;
-    CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, (hipStream_t)hip_stream));
+    CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, ctx->num_cu, (hipStream_t)hip_stream));
     return CLADA_OK;
 }
 

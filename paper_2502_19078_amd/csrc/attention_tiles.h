@@ -6,7 +6,7 @@
 // tile.  Two workgroups share a compute unit, so that one's products can run under the other's exponentials.  fp32: the same with
 // 32x32x2 products, tiles of 32 keys and weights in fp32.
 //
-// Measured (us): 8192 tokens, 32 query and 8 key heads of 128 values, window of 4096, bf16: 445 to 460 over several runs, 900 to 927 TFLOP/s on the
+// Measured (us): 8192 tokens, 32 query and 8 key heads of 128 values, window of 4096, bf16: 437 to 460 over several runs, 897 to 944 TFLOP/s on the
 // visible pairs, where a library
 // product of 8192^3 runs at 1168; a wave's tile takes 2100 clocks of its SIMD (all products together 1024): two waves do not keep
 // the matrix cores busy through each other's exponentials, LDS reads and barriers.  On the way: rows of attention_rows.h 2710; these tiles 554;

@@ -228,3 +228,16 @@ def test_same_bits_again_on_another_stream_and_in_a_graph(clada, ctx, T):
             assert torch.equal(out, want) and torch.equal(want, first) == (k == 1)
     s.synchronize()
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [900, 1024, 1025, 1160])
+def test_joins_of_many_rows(clada, ctx, dtype, cap):
+    """More than 1024 rows (four a compute unit) in eight splits and in nine and ten; sequences that leave splits, or everything, without keys."""
+    _window_case(clada, ctx, dtype, 40, 8, 8, 48, [cap, 130, 0, 48], [48, 30, 0, 47], 0, 0, cap=cap, seed=cap)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,Hq,H,B", [(80, 40, 2, 33), (256, 24, 3, 45)])
+def test_shared_prefix_joins_of_many_rows(clada, ctx, dtype, D, Hq, H, B):
+    test_shared_prefix(clada, ctx, dtype, D, Hq, H, B, 500)

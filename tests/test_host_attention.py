@@ -46,7 +46,7 @@ if __name__ != "__main__":
         (dict(do="window", B=1, T=100, Hq=4, H=4, D=80, cap=32768, dtype=0), [("tiles", 4 * 128), ("join", 400)]),
         (dict(do="prefix", B=4, Hq=8, H=2, D=64, cap=64, P=1000), [("rows", 2 * 8 + 4 * 2), ("join", 32)]),
         (dict(do="prefix", B=16, Hq=32, H=8, D=128, cap=512, P=8192), [("prefix", 8 * 32 + 128 * 2), ("join", 512)]),
-        (dict(do="prefix", B=64, Hq=32, H=8, D=128, cap=64, P=100, dtype=0), [("prefix", 8 * 2 + 512), ("join", 2048)]),
+        (dict(do="prefix", B=64, Hq=32, H=8, D=128, cap=64, P=100, dtype=0), [("prefix", 8 * 2 + 512), ("join", 2048 // 8)]),
         (dict(do="rope", B=1, T=1, Hq=32, H=8, D=128), [("qk_rope", 2)]),
         (dict(do="rope", B=1, T=4096, Hq=32, H=8, D=128), [("qk_rope", 4096 * 12 * 8 // 256)]),
         (dict(do="rope", B=2, T=300, Hq=5, H=1, D=256, dtype=0), [("qk_rope", 600 * 7 * 32 // 256)]),
