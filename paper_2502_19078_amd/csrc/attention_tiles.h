@@ -112,8 +112,13 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     const bool in = WHOLE || col < Dd * ES;
     const unsigned int lane_off = (unsigned int)first_key * (unsigned int)kv.sn + (in ? col : 0), step_off = 256 / CPR * (unsigned int)kv.sn;
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
-    // A whole tile of consecutive cache rows has one base for all lanes (offsets in 32 bits: no row further than 32 MiB from the next).
-    auto regular = [&](int i) { return i + KT <= k1 && kv.sn < (1 << 25) && kr.row(kr.pos(i + KT - 1), kv) - kr.row(kr.pos(i), kv) == KT - 1; };
+    // A whole tile of consecutive cache rows has one base for all lanes (offsets in 32 bits: no row further than 32 MiB from the next).  Its first
+    // and last row tell, except where the key behind the last sink lies elsewhere than in the row behind it: the ring may then wrap just as many
+    // rows short as the seam skips.  A tile across such a seam is never regular.
+    const int seam = kr.n > kr.head && kr.row(kr.lo, kv) != kr.head ? kr.head : 0;
+    auto regular = [&](int i) {
+        return i + KT <= k1 && (i >= seam || i + KT <= seam) && kv.sn < (1 << 25) && kr.row(kr.pos(i + KT - 1), kv) - kr.row(kr.pos(i), kv) == KT - 1;
+    };
     __amdgpu_buffer_rsrc_t k_tile, v_tile;
     auto aim = [&](int i) {                                  // at a regular tile
         const int64_t at = kr.row(kr.pos(i), kv) * kv.sn;

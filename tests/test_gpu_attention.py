@@ -241,3 +241,26 @@ def test_joins_of_many_rows(clada, ctx, dtype, cap):
 @pytest.mark.parametrize("D,Hq,H,B", [(80, 40, 2, 33), (256, 24, 3, 45)])
 def test_shared_prefix_joins_of_many_rows(clada, ctx, dtype, D, Hq, H, B):
     test_shared_prefix(clada, ctx, dtype, D, Hq, H, B, 500)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,Hq,H,T,window,sinks,n_sink,ring", [(64, 2, 2, 64, 40, 1, 3, 110), (128, 4, 1, 32, 100, 4, 8, 131), (256, 1, 1, 40, 30, 2, 7, 75),
+                                                               (96, 3, 1, 30, 60, 70, 75, 90)])
+def test_rings_with_more_rows_of_their_own_than_sinks(clada, ctx, dtype, D, Hq, H, T, window, sinks, n_sink, ring):
+    """Many rows, n_sink > sinks: a sequence of every length over a whole period of the ring, so that it wraps at every distance behind the sinks."""
+    B, G = ring, Hq // H
+    lens = [n_sink + 2 * ring + b for b in range(B)]
+    rng = np.random.default_rng(ring)
+    q = _draw(rng, dtype, B, T, Hq, D)
+    kc, vc = (_draw(rng, dtype, B, H, n_sink + ring, D) for _ in range(2))
+    out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc, n_sink, ring), _ints(lens), None, window, sinks, want_lse=True)
+    Q, K, V = to_np(q), to_np(kc), to_np(vc)
+    r = dict(out=np.zeros(Q.shape), lse=np.zeros(Q.shape[:3]), mag=np.zeros(Q.shape), S=np.zeros(Q.shape[:3]), n=np.zeros(Q.shape[:3], int))
+    for b in range(B):
+        for t in range(T):
+            pos = lens[b] - T + t
+            rows = [ref.cache_row(p, n_sink, ring) for p in sorted({*range(pos - window + 1, pos + 1), *range(sinks)})]
+            for h in range(Hq):
+                r["out"][b, t, h], r["lse"][b, t, h], r["mag"][b, t, h], r["S"][b, t, h] = ref.attend(Q[b, t, h], K[b, h // G, rows], V[b, h // G, rows], D ** -0.5)
+                r["n"][b, t, h] = len(rows)
+    ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=True)
