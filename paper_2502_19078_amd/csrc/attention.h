@@ -122,7 +122,7 @@ __device__ __forceinline__ void sequence_lens(const AttnArgs &a, int len_b, int 
 // A product over a tile gives every row every key of it, and a weight of zero (or the lower half of a weight) times a value that is not finite
 // is no zero.  A row whose outputs are not finite is therefore computed a second time by one wave, key by key as it sees them: 64 keys'
 // scores at once, a lane each, then their values one after the other, a lane for every 64th dimension.  It also serves a row whose weights
-// have outgrown fp32.  A row whose sum is NaN stays: a NaN score makes every output NaN.
+// have outgrown fp32 (attention_tiles.h).  Any other row whose sum is NaN stays: a NaN score makes every output NaN.
 struct RowAgain { float m, l, o[CLADA_ATTN_MAX_D / 64]; };
 
 template <int ES>

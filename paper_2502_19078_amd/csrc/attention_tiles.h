@@ -163,8 +163,9 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     };
 
     // A row's maximum is that of the first tile that it sees; its weights grow past 1 from there on (as floats they lose nothing) and are
-    // scaled down where a sum passes 2^60: no maxima in the loop.  Where scores rise by more than 60 powers of two within a tile, the row's
-    // sums overflow and it is computed again below.
+    // scaled down where a sum passes 2^60: no maxima in the loop.  A row whose sum has passed 2^100 by then (scores of 94 powers of two and more above
+    // those that its maximum was taken from, within a tile) is computed again below: a factor below 2^-126 is zero in the scaling and in the join of
+    // splits, which costs a sum of 2^100 a part of 2^-26 at most, but a larger one parts that count, and an infinite one is NaN behind it.
     f32x16 o[DB];
     float m = row_pos < 0 || r >= rows ? 0.0f : NEG_INF;     // (a row that sees nothing does not wait for its first key)
     float l = 0.0f;
@@ -173,6 +174,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
     bool steady = false;                                     // every row has its maximum, and no sum has passed 2^60
+    bool outgrown = false;                                   // this row's sum passed 2^100
     // One tile for this wave's rows.  EDGE: some of them do not see all of it, or a maximum has to be set or moved.  Otherwise the next tile goes
     // into LDS, and the one after it (regular, aimed at) is taken, transfer by transfer between the products: the loads of all waves pass one
     // address unit, and in one place they would hold up the waves for 800 clocks of a tile.
@@ -230,6 +232,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
             top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
             const float grown = fmaxf(l, __shfl_xor(l, 32)), mn = top > m + 8.0f ? top : grown > 0x1p60f ? m + 60.0f : m;
             if (__any(mn != m)) {
+                outgrown = outgrown || grown > 0x1p100f;
                 const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
                 m = mn;
                 l *= f;
@@ -337,13 +340,14 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
         }
     }
     l += __shfl_xor(l, 32);
-    bool fine = l < INFINITY;
+    outgrown = outgrown || l > 0x1p100f;                     // (an l that is NaN without it is a NaN score's)
+    bool fine = true;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) fine = fine && fabsf(o[d][e]) < INFINITY;
     const bool nothing = kr.n == 0 || row_pos < 0;
-    const unsigned long long odd = __ballot(!fine && !(l != l) && !nothing && r < rows);
+    const unsigned long long odd = __ballot((outgrown || (!fine && l == l)) && !nothing && r < rows);
     const unsigned int again = (unsigned int)odd | (unsigned int)(odd >> 32);      // a bit for every row of the wave
     for (unsigned int left = again; left; left &= left - 1) {
         const int t = __builtin_ctz(left);

@@ -264,3 +264,77 @@ def test_rings_with_more_rows_of_their_own_than_sinks(clada, ctx, dtype, D, Hq, 
                 r["out"][b, t, h], r["lse"][b, t, h], r["mag"][b, t, h], r["S"][b, t, h] = ref.attend(Q[b, t, h], K[b, h // G, rows], V[b, h // G, rows], D ** -0.5)
                 r["n"][b, t, h] = len(rows)
     ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=True)
+
+
+def _dense(q, k, v, scale, seen):
+    """Rows q [..][r][D] over keys k, v [n][D] where seen [r][n], in 64 bits and laid out for ref.check."""
+    k, v = k.double(), v.double()
+    kt = k.t().contiguous()
+    s = (scale * torch.matmul(q.double(), kt)).masked_fill(~seen, -float("inf"))
+    lse = torch.logsumexp(s, -1)
+    p = torch.exp(s - lse[..., None])
+    S = abs(scale) * torch.matmul(q.double().abs(), kt.abs()).masked_fill(~seen, 0.0).amax(-1)
+    r = {name: x.cpu().numpy() for name, x in dict(out=torch.matmul(p, v), lse=lse, mag=torch.matmul(p, v.abs()), S=S).items()}
+    return dict(r, n=np.broadcast_to(seen.sum(-1).cpu().numpy(), lse.shape))
+
+
+def _levels(kind, n, tile):
+    """What the scores of n keys stand around, in powers of two."""
+    x = np.zeros(n)
+    if kind.startswith("rise"):                                 # from the middle of a tile on
+        x[n // 3 + 5:] = float(kind[4:])
+    elif kind == "stairs":
+        x[n // 4:], x[n // 2:], x[3 * n // 4:] = 90, 220, 100
+    elif kind == "pair":                                        # one key, then one of four times its weight in the tile behind it
+        for a in range(3 * tile + 3, n - tile, n // 2):
+            x[a], x[a + tile] = 126, 128
+    return x
+
+
+def _rising(rng, dtype, D, n, kind):
+    """Keys and values [n][D] whose scores against a query that begins with a 4 stand around the levels of `kind`."""
+    k, v = 0.3 * _draw(rng, dtype, n, D), _draw(rng, dtype, n, D)
+    if kind == "lowest first":                                  # whole tiles of scores around -1e36: weights of exactly zero
+        k[:n // 4, 0] = -1e36
+    else:
+        k[:, 0] = torch.from_numpy(_levels(kind, n, 64 if dtype == "bf16" and D <= 128 else 32) * np.log(2.0) * D ** 0.5 / 4.0).to(DEV)
+    return k, v
+
+
+RISES = ["rise70", "rise100", "rise127", "rise200", "stairs", "pair", "lowest first"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("kind", RISES)
+@pytest.mark.parametrize("B", [8, 16])                          # with 32 key heads: keys in two splits, in one
+def test_many_rows_whose_scores_rise(clada, ctx, dtype, D, kind, B):
+    """Scores that pass those of a row's first tile by any number of powers of two, in a tile that takes no maxima or in the one behind it."""
+    rng = np.random.default_rng(D + B)
+    H, T, n = 32, 20, 1024
+    q = 0.3 * _draw(rng, dtype, B, T, H, D)
+    q[..., 0] = 4.0
+    k, v = _rising(rng, dtype, D, n, kind)
+    cache = clada.KVCache(*(x.expand(B, H, n, D) for x in (k, v)))
+    out, lse = clada.window_attn(ctx, q, cache, _ints([n] * B), want_lse=True)
+    seen = torch.arange(n, device=DEV) <= torch.arange(n - T, n, device=DEV)[:, None]
+    use = slice(n // 4 if kind == "lowest first" else 0, n)
+    r = _dense(q.transpose(1, 2), k[use], v[use], D ** -0.5, seen[:, use])
+    ref.check(to_np(out.transpose(1, 2)), to_np(lse.transpose(1, 2)), r, dtype, weights_bf16=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("kind", RISES)
+def test_a_shared_prefix_whose_scores_rise(clada, ctx, dtype, D, kind):
+    """The same behind more than 16 rows a key head: eight splits of 512 rows whose sums stand at different powers of two."""
+    rng = np.random.default_rng(D)
+    B, H, n = 40, 32, 4096
+    q = 0.3 * _draw(rng, dtype, B, H, D)
+    q[..., 0] = 4.0
+    k, v = _rising(rng, dtype, D, n, kind)
+    cache = clada.KVCache(*(x[:1].expand(B, H, 1, D) for x in (k, v)))
+    out, lse = clada.shared_prefix_attn(ctx, q, clada.KVCache(*(x.expand(1, H, n, D) for x in (k, v))), n, cache, _ints([0] * B), want_lse=True)
+    use = slice(n // 4 if kind == "lowest first" else 0, n)
+    r = _dense(q, k[use], v[use], D ** -0.5, torch.ones(1, n, dtype=torch.bool, device=DEV)[:, use])
+    ref.check(to_np(out), to_np(lse), r, dtype)
