@@ -421,7 +421,9 @@ clada_status clada_static_ffn_decode(clada_ctx *ctx, const clada_layer *layer, c
  *
  * clada_heads: a view [B][T][H][d] of queries, keys, values or outputs; strides in elements, the d values of a head
  * contiguous.  clada_kv_cache: keys and values [batch][heads][capacity][d] of one shape and one set of strides.  Pointers and
- * strides are multiples of 16 bytes, strides are not negative (an input may have strides of 0); d is a multiple of 8.
+ * strides are multiples of 16 bytes, strides are not negative; d is a multiple of 8.  An input may have strides of 0 (or below d).  The heads of an
+ * output, and the rows that a call stores into, must not overlap: a stride below d along more than one of them is refused
+ * (CLADA_ERR_SHAPE; between the sequences of a cache it is not, their tokens may go to different rows).
  * Without a ring (ring = 0) row n of a cache holds the token at position n.  With one, positions below n_sink have their own
  * rows and a later position p lies in row n_sink + (p - n_sink) % ring, where it replaces position p - ring.  Keys are
  * stored rotated, so attention does not mind the order of rows. */

@@ -32,6 +32,15 @@ clada_status clada_check_heads(clada_ctx *ctx, const clada_heads *h, int32_t dty
     return CLADA_OK;
 }
 
+clada_status clada_check_out(clada_ctx *ctx, const clada_heads *h, int32_t dtype, int32_t B, int32_t T, int32_t H, int32_t d, const char *what)
+{
+    const clada_status st = clada_check_heads(ctx, h, dtype, what);
+    if (st != CLADA_OK) return st;
+    if ((B > 1 && h->stride_b < d) || (T > 1 && h->stride_t < d) || (H > 1 && h->stride_h < d))
+        return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: a stride below %d values puts heads on top of each other", what, d);
+    return CLADA_OK;
+}
+
 namespace {
 
 constexpr int MAX_SPLITS = 256;                              // of one row's keys
@@ -140,7 +149,7 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
         return clada_fail(ctx, CLADA_ERR_SHAPE, "a ring of %d rows behind %d does not hold a window of %d for %d queries and %d sinks", cache->ring,
                           cache->n_sink, window, T, sinks);
     if ((st = clada_check_heads(ctx, q, cache->dtype, "q")) != CLADA_OK) return st;
-    if ((st = clada_check_heads(ctx, out, cache->dtype, "out")) != CLADA_OK) return st;
+    if ((st = clada_check_out(ctx, out, cache->dtype, B, T, Hq, cache->d, "out")) != CLADA_OK) return st;
     if (ctx->ws_bytes == 0) return clada_fail(ctx, CLADA_ERR_WORKSPACE, "context has no device");
 
     AttnArgs a = {};
@@ -182,7 +191,7 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     if (prefix_len < 1 || prefix_len > prefix->capacity)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "prefix_len=%d outside [1,%d]", prefix_len, prefix->capacity);
     if ((st = clada_check_heads(ctx, q, cache->dtype, "q")) != CLADA_OK) return st;
-    if ((st = clada_check_heads(ctx, out, cache->dtype, "out")) != CLADA_OK) return st;
+    if ((st = clada_check_out(ctx, out, cache->dtype, B, 1, Hq, cache->d, "out")) != CLADA_OK) return st;
     if (ctx->ws_bytes == 0) return clada_fail(ctx, CLADA_ERR_WORKSPACE, "context has no device");
 
     AttnArgs a = {};

@@ -74,6 +74,7 @@ static inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; 
 clada_status clada_check_layer(clada_ctx *ctx, const clada_layer *layer);
 clada_status clada_check_kv(clada_ctx *ctx, const clada_kv_cache *c, const char *what, bool data);
 clada_status clada_check_heads(clada_ctx *ctx, const clada_heads *h, int32_t dtype, const char *what);
+clada_status clada_check_out(clada_ctx *ctx, const clada_heads *h, int32_t dtype, int32_t B, int32_t T, int32_t H, int32_t d, const char *what);
 clada_status clada_require_swiglu(clada_ctx *ctx, const clada_layer *layer, const char *call);
 
 // Batched (B >= 2, bf16) MFMA decode path; *ran tells whether the shape was eligible and it ran.

@@ -298,6 +298,8 @@ extern "C" clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, co
         return clada_fail(ctx, CLADA_ERR_SHAPE, "B=%d, T=%d: need B in [1,%d], T >= 1 and B*T <= %d", B, T, CLADA_ATTN_MAX_BATCH, CLADA_ATTN_MAX_ROWS);
     if (q && (Hq < 1 || Hq > CLADA_ATTN_MAX_HEADS)) return clada_fail(ctx, CLADA_ERR_SHAPE, "Hq=%d outside [1,%d]", Hq, CLADA_ATTN_MAX_HEADS);
     if (k && cache->batch < B) return clada_fail(ctx, CLADA_ERR_SHAPE, "the cache holds %d sequences, the call has %d", cache->batch, B);
+    if (k && ((cache->heads > 1 && cache->stride_h < cache->d) || (T > 1 && cache->capacity > 1 && cache->stride_n < cache->d)))
+        return clada_fail(ctx, CLADA_ERR_SHAPE, "cache: a stride below %d values puts what is stored on top of each other", cache->d);
     if (k && !slots && cache->ring && T > cache->ring)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%d tokens a sequence do not fit a ring of %d rows", T, cache->ring);
     const int R = rope->rotary_dim;
@@ -309,7 +311,7 @@ extern "C" clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, co
     if ((((uintptr_t)positions | (uintptr_t)slots) & 3u) || !aligned16(rope->turns) || (norm && (!aligned16(norm->q_weight) || !aligned16(norm->k_weight))))
         return clada_fail(ctx, CLADA_ERR_ALIGN, "turns and weights must be 16-byte, positions and slots 4-byte aligned");
     if (q && (st = clada_check_heads(ctx, q, cache->dtype, "q")) != CLADA_OK) return st;
-    if (q && (st = clada_check_heads(ctx, q_out, cache->dtype, "q_out")) != CLADA_OK) return st;
+    if (q && (st = clada_check_out(ctx, q_out, cache->dtype, B, T, Hq, cache->d, "q_out")) != CLADA_OK) return st;
     if (k && (st = clada_check_heads(ctx, k, cache->dtype, "k")) != CLADA_OK) return st;
     if (k && (st = clada_check_heads(ctx, v, cache->dtype, "v")) != CLADA_OK) return st;
     if (ctx->ws_bytes == 0) return clada_fail(ctx, CLADA_ERR_WORKSPACE, "context has no device");

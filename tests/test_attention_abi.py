@@ -141,3 +141,24 @@ def test_turns_are_the_frequencies(b, kind, R, theta):
 def test_the_binding_refuses_host_tensors(b):
     with pytest.raises(AssertionError):
         b.KVCache(torch.zeros(1, 1, 4, 64), torch.zeros(1, 1, 4, 64))
+
+
+def test_outputs_on_top_of_each_other_are_refused(b):
+    """A stride of 0, or below the values of a head, along a dimension of more than one: for outputs and for what is stored, not for inputs."""
+    c = Calls(b)
+    low = dict(stride_b=0), dict(stride_t=64), dict(stride_h=0), dict(stride_h=120)
+    for s in low:
+        assert c.qk_rope(out=s) == c.window(out=s, T=3) == SHAPE, s
+        assert c.qk_rope(q=s, k=s, v=s) == c.window(q=s, T=3) == c.prefix(q=s) == WORKSPACE, s
+    assert c.window(out=low[0]) == SHAPE and b"on top of each other" in c.lib.clada_last_error(c.h)
+    for s in (low[0], low[2], low[3]):
+        assert c.prefix(out=s) == SHAPE, s
+    # a dimension of one row has no stride to speak of
+    assert c.window(out=dict(stride_b=0, stride_t=0, stride_h=0), B=1, T=1, Hq=1, cache=dict(heads=1)) == WORKSPACE
+    assert c.window(out=dict(stride_t=0)) == c.prefix(out=dict(stride_t=0)) == WORKSPACE
+    assert c.qk_rope(out=dict(stride_b=0, stride_t=0, stride_h=0), B=1, T=1, Hq=1) == WORKSPACE
+    # the cache: read with any strides, stored into with rows and heads of their own
+    for s in (dict(stride_h=0), dict(stride_h=64), dict(stride_n=0), dict(stride_n=64)):
+        assert c.qk_rope(cache=s) == SHAPE and c.qk_rope(cache=s, k=None, v=None) == c.window(cache=s) == c.prefix(cache=s) == c.prefix(prefix=s) == WORKSPACE, s
+    assert c.qk_rope(cache=dict(stride_b=0), slots=c.p) == c.qk_rope(cache=dict(stride_n=0), T=1) == c.qk_rope(cache=dict(stride_n=0, capacity=1)) == WORKSPACE
+    c.lib.clada_destroy(c.h)
