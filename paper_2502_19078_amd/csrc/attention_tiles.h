@@ -96,7 +96,7 @@ __device__ __forceinline__ void attn_tiles(const AttnArgs &a, const bool pre, co
     const bool ragged = !pre && wr1 / a.G >= qlen;           // rows of padding among them
 
     const unsigned int flip = a.scale2 < 0.0f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;      // a negative scale is the queries' sign
-    const float scale2 = fmaxf(fabsf(a.scale2), 1e-37f);     // (positive, so that -inf stays what it is)
+    const float scale2 = fmaxf(fabsf(a.scale2), 0x1p-149f);  // positive, so that -inf stays what it is (2^128, the largest product, counts 2^-21)
     u32x4 qf[KD];
 #pragma unroll
     for (int c = 0; c < KD; ++c) {

@@ -338,3 +338,17 @@ def test_a_shared_prefix_whose_scores_rise(clada, ctx, dtype, D, kind):
     use = slice(n // 4 if kind == "lowest first" else 0, n)
     r = _dense(q, k[use], v[use], D ** -0.5, torch.ones(1, n, dtype=torch.bool, device=DEV)[:, use])
     ref.check(to_np(out), to_np(lse), r, dtype)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("scale", [0.0, 1e-38, -1e-39])
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_scale_of_next_to_nothing(clada, ctx, dtype, T, scale, D):
+    """Products of 1e37 and a scale that leaves nothing of them, or a few tenths: a float of 2^-149ths, 12 u of 1e-39, well within the d u of a score."""
+    rng = np.random.default_rng(T)
+    n = 200
+    q, kc, vc = 2e18 * _draw(rng, dtype, 1, T, 2, D), 1e18 * _draw(rng, dtype, 1, 1, n, D), _draw(rng, dtype, 1, 1, n, D)
+    out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n]), scale=scale, want_lse=True)
+    r = ref.window_attn(to_np(q), to_np(kc), to_np(vc), [n], [T], 0, 0, scale)
+    ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=True)
