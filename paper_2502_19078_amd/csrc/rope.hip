@@ -167,7 +167,7 @@ k_qk_rope(const RopeArgs a)
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int e = 0; e < E; ++e) ss = fmaf(x[k][e], x[k][e], ss);
-                    r = __builtin_amdgcn_rsqf(fmaf(group_sum<LG>(ss), a.inv_d, a.eps));
+                    r = rsqrtf(fmaf(group_sum<LG>(ss), a.inv_d, a.eps));      // (the bare instruction takes a subnormal mean for 0)
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {

@@ -150,3 +150,18 @@ def test_many_tokens_and_heads(clada, ctx, T):
     _check(to_np(out), to_np(q), pos.cpu().numpy(), f, "half", 1.0, None, None, 0.0, "bf16")
     _check(to_np(kc.transpose(1, 2)), to_np(k), pos.cpu().numpy(), f, "half", 1.0, None, None, 0.0, "bf16")
     assert torch.equal(vc.transpose(1, 2), v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_a_norm_of_values_whose_squares_are_subnormal(clada, ctx, dtype, layout):
+    """eps = 0 and heads of +-2^-64: the mean square 2^-128 is exact and below fp32's normal numbers; the normed values are +-1."""
+    D = 64
+    plan = clada.rope_plan(ctx, D, layout=clada.ROPE_HALF if layout == "half" else clada.ROPE_PAIRS)
+    pos = torch.tensor([[0, 3, 70]], dtype=torch.int32, device=DEV)
+    cache = clada.KVCache(*(torch.zeros(1, 1, 1, D, dtype=_draw(1, dtype, 1).dtype, device=DEV) for _ in range(2)))
+    q = torch.sign(_draw(1, dtype, 1, 3, 5, D)) * 2.0 ** -64
+    w = _draw(2, dtype, D)
+    f, _ = ref.frequencies(D)
+    out = clada.qk_rope(ctx, plan, q, None, None, pos, cache, q_norm=w, eps=0.0)
+    _check(to_np(out), to_np(q), pos.cpu().numpy(), f, layout, 1.0, to_np(w), 0.0, 0.0, dtype)
