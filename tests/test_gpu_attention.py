@@ -352,3 +352,27 @@ def test_a_scale_of_next_to_nothing(clada, ctx, dtype, T, scale, D):
     out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints([n]), scale=scale, want_lse=True)
     r = ref.window_attn(to_np(q), to_np(kc), to_np(vc), [n], [T], 0, 0, scale)
     ref.check(to_np(out), to_np(lse), r, dtype, weights_bf16=True)
+
+
+@pytest.mark.parametrize("D,Hq,H,B", [(128, 8, 2, 3), (64, 4, 4, 1), (80, 5, 5, 17), (256, 8, 1, 5), (96, 6, 3, 40), (64, 40, 2, 2), (128, 16, 1, 64)])
+@pytest.mark.parametrize("P", [1, 31, 500])
+def test_a_shared_prefix_keeps_two_bf16_of_a_weight(clada, ctx, D, Hq, H, B, P):
+    """The bound of weights of 16 bits, on few rows and on many."""
+    rng = np.random.default_rng(D + B + P)
+    q, lens = _draw(rng, "bf16", B, Hq, D), [int(v) for v in rng.integers(0, 41, B)]
+    pk, pv = (_draw(rng, "bf16", 1, H, P, D) for _ in range(2))
+    kc, vc = (_draw(rng, "bf16", B, H, 40, D) for _ in range(2))
+    out, lse = clada.shared_prefix_attn(ctx, q, clada.KVCache(pk, pv), P, clada.KVCache(kc, vc), _ints(lens), want_lse=True)
+    ref.check(to_np(out), to_np(lse), ref.shared_prefix_attn(to_np(q), to_np(pk)[0], to_np(pv)[0], P, to_np(kc), to_np(vc), lens, D ** -0.5), "bf16")
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 200])
+@pytest.mark.parametrize("T,Hq,H", [(2, 1, 1), (4, 8, 2), (16, 3, 3), (2, 8, 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_up_to_sixteen_rows_keep_two_bf16_of_a_weight(clada, ctx, D, T, Hq, H, window, sinks):
+    """Several queries, at most 16 rows a key head: the bound of weights of 16 bits."""
+    rng = np.random.default_rng(D + T)
+    lens, cap = [T, T + 100, T + 31, 330], 330
+    q, kc, vc = _draw(rng, "bf16", 4, T, Hq, D), _draw(rng, "bf16", 4, H, cap, D), _draw(rng, "bf16", 4, H, cap, D)
+    out, lse = clada.window_attn(ctx, q, clada.KVCache(kc, vc), _ints(lens), None, window, sinks, want_lse=True)
+    ref.check(to_np(out), to_np(lse), ref.window_attn(to_np(q), to_np(kc), to_np(vc), lens, [T] * 4, window, sinks, D ** -0.5), "bf16")
