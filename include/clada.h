@@ -502,8 +502,11 @@ size_t clada_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t d);
  * Query head h reads key head h / (Hq / heads).  A query that sees nothing (a row past q_lens[b], a negative position) gives zeros
  * and an lse of -inf.  T = 1 is a decode step, T = lens a prompt.  Without a ring lens[b] <= capacity (more is taken as capacity);
  * with one, window >= 1, ring >= window + T - 1 and sinks <= n_sink.  Cache rows that a query does not see do not reach its output,
- * whatever they hold.  out must not overlap q.  Scores, sums and outputs are accumulated in fp32; the weights of bf16 calls enter the product
- * with v as one bf16 (T > 1 and more than 16 rows T Hq / heads) or as two.  Bit-reproducible from run to run. */
+ * whatever they hold.  out must not overlap q.  Scores, sums and outputs are accumulated in fp32 (values whose weighted sum leaves fp32's
+ * range give infinities, also where their mean would not); the weights of bf16 calls enter the product
+ * with v as one bf16 (T > 1 and more than 16 rows T Hq / heads) or as two.  Bit-reproducible from run to run.
+ * A row beside whose own keys a value that is not finite is read for other rows, and on more than 16 rows one whose scores rise by 94 powers of two or
+ * more within 64 keys, is computed a second time by itself: right, but hundreds of times slower. */
 clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada_kv_cache *cache, const int32_t *lens,
                                const int32_t *q_lens, int32_t B, int32_t T, int32_t Hq, int32_t window, int32_t sinks, float scale,
                                const clada_heads *out, float *lse, void *hip_stream);

@@ -25,7 +25,7 @@ k_attn_tiles(const AttnArgs a)
 }
 
 // A shared prefix for more than 16 rows: its workgroups first, then those of the sequences' own keys, in one launch.  Bound by the bytes of both:
-// 16 sequences behind 8192 rows, 8 key heads of 128 values, 20 us (2.6 TB/s with the join); 48 behind 4095, 32 key heads, 38 (3.4).  Tiles
+// 16 sequences behind 8192 rows, 8 key heads of 128 values, 21 us (2.5 TB/s with the join); 48 behind 4095, 32 key heads, 39 (3.3).  Tiles
 // of 32 rows in attention_rows.h, which read the prefix once for every 32 rows, took 48 and 93.
 template <int ES, int DP, bool FULL>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)

