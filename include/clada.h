@@ -490,7 +490,7 @@ clada_status clada_qk_rope(clada_ctx *ctx, const clada_rope *rope, const clada_h
                            const clada_heads *q, const clada_heads *k, const clada_heads *v, const int32_t *positions,
                            const int32_t *slots, const clada_heads *q_out, const clada_kv_cache *cache, void *hip_stream);
 
-/* Upper bound of the workspace the two attention calls make use of (beside clada_workspace_bytes: a context for both needs the
+/* Upper bound of the workspace the attention calls make use of (beside clada_workspace_bytes: a context for both needs the
  * larger of the two). */
 size_t clada_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t d);
 
@@ -518,6 +518,71 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
 clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, const clada_kv_cache *prefix, int32_t prefix_len,
                                       const clada_kv_cache *cache, const int32_t *lens, int32_t B, int32_t Hq, float scale,
                                       const clada_heads *out, float *lse, void *hip_stream);
+
+/* ---- A paged cache: rows of `page_size` positions from a pool that all sequences share, in 32, 16 or 4 bits a value.
+ *
+ * Position p of sequence b lies in row p % page_size of page table[b][p / page_size].  An entry outside [0, pages) names no page: its
+ * positions are not stored, read as zeros, and are seen by no query; so are positions from max_pages * page_size on.  Sequences may share
+ * pages that no call stores into.  k and v are [pages][heads][page_size][d] of one set of strides (elements; multiples of 16 bytes, 32
+ * values for CLADA_PAGE_MX4), the d values of a row contiguous; page_size is a power of two from 16 to 4096; table (device) has rows of
+ * table_stride entries.
+ *
+ * CLADA_PAGE_MX4 holds a value in 4 bits (d a multiple of 32): 32 neighbours of a row share a power of two, 2^(byte - 127) with one byte in
+ * k_scales / v_scales (byte 255: all 32 are NaN), and a value is 0, 0.5, 1, 1.5, 2, 3, 4 or 6 of it, codes 0 to 7, with 8 added for a
+ * minus; the lower of two neighbours lies in the lower half of a byte.  That is 17 bytes for 32 values, each exact in bf16; queries, new
+ * rows and outputs are bf16.  k and v have d/2 bytes a row, and the scales lie alike: the byte for the element at offset i of k
+ * is k_scales[i / 32].  A block is stored with the power of two 2^(e - 2) where its largest magnitude is in [2^e, 1.75 2^e), twice that above
+ * (2^-126 at least, 2^125 at most); values go to the nearest code, ties to the even one, 6 the largest.  A block that holds a value that is not finite is stored as NaN. */
+typedef enum { CLADA_PAGE_F32 = 0, CLADA_PAGE_BF16 = 1, CLADA_PAGE_MX4 = 2 } clada_page_type;
+#define CLADA_PAGE_MIN 16
+#define CLADA_PAGE_MAX 4096
+typedef struct {
+    void *k, *v;
+    uint8_t *k_scales, *v_scales;           /* CLADA_PAGE_MX4 only, ignored otherwise */
+    int64_t stride_p, stride_h, stride_n;   /* elements: page, head, row; the same for k and v */
+    const int32_t *table;                   /* [batch][max_pages] */
+    int64_t table_stride;
+    int32_t pages, heads, page_size, d;
+    int32_t batch, max_pages;               /* max_pages * page_size <= CLADA_ATTN_MAX_CAPACITY */
+    int32_t type;                           /* a clada_page_type: queries, new rows and outputs are fp32 for CLADA_PAGE_F32, else bf16 */
+} clada_paged_cache;
+
+/* clada_qk_rope into pages: the same arguments, norm, rotation and rounding; token (b, t) is stored at positions[b][t] of sequence b (negative:
+ * padding), keys and values of CLADA_PAGE_MX4 rounded once, from fp32, to 4 bits.  The rows that a call stores into must be distinct. */
+clada_status clada_paged_rope(clada_ctx *ctx, const clada_rope *rope, const clada_head_norm *norm, int32_t B, int32_t T, int32_t Hq,
+                              const clada_heads *q, const clada_heads *k, const clada_heads *v, const int32_t *positions,
+                              const clada_heads *q_out, const clada_paged_cache *cache, void *hip_stream);
+
+/* Rows out of their pages: k_out and v_out [B][T][heads][d] (either may be NULL) receive position positions[b][t] of sequence b, a negative
+ * one and one without a page zeros.  With a row's position and strides of a contiguous cache this fills, for example, the prefix that
+ * clada_shared_prefix_attn reads. */
+clada_status clada_paged_read(clada_ctx *ctx, const clada_paged_cache *cache, const int32_t *positions, int32_t B, int32_t T,
+                              const clada_heads *k_out, const clada_heads *v_out, void *hip_stream);
+
+/* What is done to the scores of an attention call, and which keys a query sees.  Query at position pos of sequence b (query t of the call),
+ * key at position p:
+ *   x = scale q . k;   x = cap tanh(x / cap) where cap > 0;   x = x - slopes[head] |pos - p| where slopes are given;
+ *   seen where  p <= pos  or  p < prefix_lens[b] (a prefix that is seen from both sides),
+ *   and         p > pos - window  or  window = 0,   and   p >= first[b][t] (the first position of the query's document). */
+typedef struct {
+    float scale;
+    float cap;                              /* 0: none */
+    const float *slopes;                    /* device [Hq] or NULL */
+    const int32_t *prefix_lens;             /* device [B] or NULL */
+    const int32_t *first;                   /* device [B][T] or NULL */
+    int32_t window;
+} clada_attn_scores;
+
+/* Attention over a paged cache: clada_window_attn's queries, lengths, positions and outputs (query t has position lens[b] - q_lens[b] + t; a query that
+ * sees nothing, or only scores of -infinity, gives zeros and an lse of -inf), with the scores and the sight of clada_attn_scores.
+ * max_len is what the caller knows about lens, which splits long sequences among workgroups: no entry is above it (more is taken as it); 0: as
+ * much as the table has room for.  The workspace is that of clada_attn_workspace_bytes.  Pages that a query does not see do not reach its
+ * output, whatever they hold.  The weights of bf16 and 4-bit calls enter the product with v as in clada_window_attn.  Bit-reproducible from
+ * run to run.  A row beside whose own keys a value that is not finite is read for other rows is computed a second time by itself: right, but
+ * hundreds of times slower. */
+clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, const clada_paged_cache *cache, const int32_t *lens,
+                              const int32_t *q_lens, int32_t B, int32_t T, int32_t Hq, int32_t max_len, const clada_attn_scores *scores,
+                              const clada_heads *out, float *lse, void *hip_stream);
 
 /* One decode step as a replayable HIP graph (the algorithm "CLADA Inference", generation
  * phase, is the same short sequence of calls for every token: signals, thresholds, one

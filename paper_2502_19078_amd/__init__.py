@@ -16,5 +16,6 @@ from .binding import (Context, Layer, PrefixStats, CladaError, cognitive_signals
                       dense_ffn_stack_decode, layer_array,
                       workspace_bytes, Graph, graph_begin, graph_end,
                       KVCache, RopePlan, rope_plan, qk_rope, window_attn, shared_prefix_attn,
-                      attn_workspace_bytes, ROPE_HALF, ROPE_PAIRS, ROPE_SCALE_NONE, ROPE_SCALE_LINEAR,
+                      attn_workspace_bytes, PagedCache, paged_rope, paged_read, paged_attn,
+                      PAGE_F32, PAGE_BF16, PAGE_MX4, ROPE_HALF, ROPE_PAIRS, ROPE_SCALE_NONE, ROPE_SCALE_LINEAR,
                       ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP)

@@ -51,6 +51,18 @@ class _CKvCache(C.Structure):
                 ("n_sink", C.c_int32), ("ring", C.c_int32)]
 
 
+class _CPagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("stride_p", C.c_int64),
+                ("stride_h", C.c_int64), ("stride_n", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int64), ("pages", C.c_int32),
+                ("heads", C.c_int32), ("page_size", C.c_int32), ("d", C.c_int32), ("batch", C.c_int32), ("max_pages", C.c_int32), ("type", C.c_int32)]
+
+
+class _CAttnScores(C.Structure):
+    _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p), ("prefix_lens", C.c_void_p), ("first", C.c_void_p),
+                ("window", C.c_int32)]
+
+
+PAGE_F32, PAGE_BF16, PAGE_MX4 = 0, 1, 2      # clada_page_type
 ROPE_HALF, ROPE_PAIRS = 0, 1       # clada_rope_layout
 ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP = range(5)      # clada_rope_scale
 
@@ -134,13 +146,17 @@ def load_library() -> C.CDLL:
     lib.clada_qk_rope.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.clada_window_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]
     lib.clada_shared_prefix_attn.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, f32, vp, vp, vp]
+    lib.clada_paged_rope.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.clada_paged_read.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.clada_paged_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
     lib.clada_attn_workspace_bytes.argtypes = [i32] * 4
     lib.clada_attn_workspace_bytes.restype = C.c_size_t
     for name in ("clada_diag_stream_read", "clada_diag_copy", "clada_diag_kernel_times", "clada_device_fault",
                  "clada_threshold_search_cett", "clada_cett_eval", "clada_static_mask_threshold",
                  "clada_static_mask_topk", "clada_static_ffn_decode", "clada_mask_pack", "clada_mask_unpack", "clada_create", "clada_set_option", "clada_prefix_stats", "clada_threshold_calibrate",
                  "clada_cognitive_signals", "clada_threshold", "clada_signals_threshold", "clada_sparse_ffn_decode",
-                 "clada_dense_ffn_decode", "clada_rope_turns", "clada_qk_rope", "clada_window_attn", "clada_shared_prefix_attn"):
+                 "clada_dense_ffn_decode", "clada_rope_turns", "clada_qk_rope", "clada_window_attn", "clada_shared_prefix_attn", "clada_paged_rope",
+                 "clada_paged_read", "clada_paged_attn"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -595,11 +611,8 @@ def rope_plan(ctx: Context, rotary_dim: int, theta: float = 10000.0, layout: int
     return RopePlan(host.to(f"cuda:{ctx.device}"), layout, m.value)
 
 
-def qk_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
-            cache: KVCache, slots: torch.Tensor | None = None, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None,
-            eps: float = 1e-6, norm_offset: float = 0.0, norm: bool | None = None, out: torch.Tensor | None = None):
-    """Norm for each head (norm None: where a weight is given; True without weights: the bare norm), rotation, and keys and values into the cache.  q [B][T][Hq][d], k and v
-    [B][T][heads][d] (any strides, d contiguous), positions [B][T] int32 -> rotated queries (None without q)."""
+def _rope_args(plan: RopePlan, q, k, v, cache, q_norm, k_norm, eps, norm_offset, norm, out):
+    """What qk_rope and paged_rope hand to the library, checked against the cache."""
     x = q if q is not None else k
     shape = x.shape
     B, T, Hq, _ = shape
@@ -620,8 +633,16 @@ def qk_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tenso
         for w in (q_norm, k_norm):
             assert w is None or (w.get_device() == cache.device_index and w.dtype is cache.dtype and w.is_contiguous() and w.numel() == cache.d)
         c_norm = C.byref(_CHeadNorm(_ptr(q_norm), _ptr(k_norm), eps, norm_offset))
-    ctx.check(ctx._lib.clada_qk_rope(ctx._h, C.byref(_CRope(turns.data_ptr(), 2 * turns.numel(), plan.layout, plan.magnitude)), c_norm, B, T, Hq, cq,
-                                     ck, cv, _ints(positions, B * T, cache, "positions"),
+    return (x, out, B, T, Hq, C.byref(_CRope(turns.data_ptr(), 2 * turns.numel(), plan.layout, plan.magnitude)), c_norm, cq, ck, cv, co)
+
+
+def qk_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
+            cache: KVCache, slots: torch.Tensor | None = None, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None,
+            eps: float = 1e-6, norm_offset: float = 0.0, norm: bool | None = None, out: torch.Tensor | None = None):
+    """Norm for each head (norm None: where a weight is given; True without weights: the bare norm), rotation, and keys and values into the cache.  q [B][T][Hq][d], k and v
+    [B][T][heads][d] (any strides, d contiguous), positions [B][T] int32 -> rotated queries (None without q)."""
+    x, out, B, T, Hq, plan_c, norm_c, cq, ck, cv, co = _rope_args(plan, q, k, v, cache, q_norm, k_norm, eps, norm_offset, norm, out)
+    ctx.check(ctx._lib.clada_qk_rope(ctx._h, plan_c, norm_c, B, T, Hq, cq, ck, cv, _ints(positions, B * T, cache, "positions"),
                                      None if slots is None else _ints(slots, B * T, cache, "slots"), co, cache._ref, _stream(x)))
     return out if q is not None else None
 
@@ -658,6 +679,83 @@ def shared_prefix_attn(ctx: Context, q: torch.Tensor, prefix: KVCache, prefix_le
     ctx.check(ctx._lib.clada_shared_prefix_attn(ctx._h, _heads(q.unsqueeze(1), shape, cache, "q"), prefix._ref, prefix_len, cache._ref,
                                                 _ints(lens, B, cache, "lens"), B, Hq, D ** -0.5 if scale is None else scale,
                                                 _heads(out.unsqueeze(1), shape, cache, "out"), _ptr(lse), _stream(q)))
+    return (out, lse) if want_lse else out
+
+
+class PagedCache:
+    """Pages [pages][heads][page_size][d] of a pool on the GPU (k and v: views with one set of strides, d contiguous), fp32 or bf16, or in 4 bits: k and v
+    uint8 [..][d/2] with scales uint8 [..][d/32], whose strides are those of the values over 32.  table [batch][max_pages] int32 (rows contiguous) names
+    the pages of every sequence; an entry outside the pool names none."""
+    __slots__ = ("k", "v", "k_scales", "v_scales", "table", "heads", "d", "dtype", "device_index", "_c", "_ref")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None):
+        shape, stride, four = k.shape, k.stride(), k.dtype is torch.uint8
+        assert k.is_cuda and len(shape) == 4 and v.shape == shape and v.dtype is k.dtype and v.get_device() == k.get_device()
+        assert stride[3] == 1 and v.stride() == stride, "k and v need one set of strides, the values of a row contiguous"
+        assert table.dtype is torch.int32 and table.dim() == 2 and table.stride(1) == 1 and table.get_device() == k.get_device()
+        P, H, S, D = shape
+        sizes = [stride[0] if P > 1 else 0, stride[1] if H > 1 else 0, stride[2]]
+        if four:
+            assert D % 16 == 0, "rows of 4 bits hold a multiple of 32 values"
+            for x in (k_scales, v_scales):
+                assert x is not None and x.dtype is torch.uint8 and x.shape == (P, H, S, D // 16) and x.get_device() == k.get_device()
+                assert all(n == 1 or 16 * a == b for n, a, b in zip((P, H, S), x.stride(), stride)) and x.stride(3) == 1, \
+                    "the scales need the strides of the values over 32"
+            sizes, D = [2 * n for n in sizes], 2 * D
+        else:
+            assert k_scales is None and v_scales is None
+        self.k, self.v, self.k_scales, self.v_scales, self.table = k, v, k_scales, v_scales, table
+        self.heads, self.d, self.device_index = H, D, k.get_device()
+        self.dtype = torch.bfloat16 if four else k.dtype          # of queries, new rows and outputs
+        B, per = table.shape
+        self._c = _CPagedCache(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), *sizes, table.data_ptr(), table.stride(0) if B > 1 else per,
+                               P, H, S, D, B, per, PAGE_MX4 if four else PAGE_F32 if _dtype_code(k) == F32 else PAGE_BF16)
+        self._ref = C.byref(self._c)
+
+
+def paged_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
+               cache: PagedCache, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6, norm_offset: float = 0.0,
+               norm: bool | None = None, out: torch.Tensor | None = None):
+    """qk_rope into pages: token (b, t) is stored at positions[b][t] of sequence b (negative: padding)."""
+    x, out, B, T, Hq, plan_c, norm_c, cq, ck, cv, co = _rope_args(plan, q, k, v, cache, q_norm, k_norm, eps, norm_offset, norm, out)
+    ctx.check(ctx._lib.clada_paged_rope(ctx._h, plan_c, norm_c, B, T, Hq, cq, ck, cv, _ints(positions, B * T, cache, "positions"), co, cache._ref, _stream(x)))
+    return out if q is not None else None
+
+
+def paged_read(ctx: Context, cache: PagedCache, positions: torch.Tensor, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
+    """Keys and values [B][T][heads][d] of positions [B][T] int32, each in its sequence (negative, or without a page: zeros).  Without outputs
+    both are made; with one of them that one alone is read."""
+    shape = (*positions.shape, cache.heads, cache.d)
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.empty(shape, dtype=cache.dtype, device=positions.device) for _ in range(2))
+    for x in (k_out, v_out):
+        assert x is None or x.shape == shape
+    B, T = positions.shape
+    ctx.check(ctx._lib.clada_paged_read(ctx._h, cache._ref, _ints(positions, B * T, cache, "positions"), B, T,
+                                        None if k_out is None else _heads(k_out, shape, cache, "k_out"),
+                                        None if v_out is None else _heads(v_out, shape, cache, "v_out"), _stream(positions)))
+    return k_out, v_out
+
+
+def paged_attn(ctx: Context, q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_lens: torch.Tensor | None = None, max_len: int = 0,
+               window: int = 0, scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None,
+               prefix_lens: torch.Tensor | None = None, first: torch.Tensor | None = None, out: torch.Tensor | None = None, want_lse: bool = False):
+    """Attention of q [B][T][Hq][d] over paged sequences; lens, q_lens, window and the results as in window_attn.  cap > 0: scores x become
+    cap tanh(x / cap); slopes [Hq] fp32: less slopes[h] a position of distance; prefix_lens [B] int32: positions below are seen by
+    the queries ahead of them too; first [B][T] int32: the first position that a query sees.  max_len: no entry of lens is above it (0: not known)."""
+    shape = q.shape
+    B, T, Hq, D = shape
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        assert out.shape == shape
+    assert slopes is None or (slopes.dtype is torch.float32 and slopes.numel() == Hq and slopes.is_contiguous() and slopes.get_device() == cache.device_index)
+    lse = torch.empty((B, T, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    c = _CAttnScores(D ** -0.5 if scale is None else scale, cap, _ptr(slopes), None if prefix_lens is None else _ints(prefix_lens, B, cache, "prefix_lens"),
+                     None if first is None else _ints(first, B * T, cache, "first"), window)
+    ctx.check(ctx._lib.clada_paged_attn(ctx._h, _heads(q, shape, cache, "q"), cache._ref, _ints(lens, B, cache, "lens"),
+                                        None if q_lens is None else _ints(q_lens, B, cache, "q_lens"), B, T, Hq, max_len, C.byref(c),
+                                        _heads(out, shape, cache, "out"), _ptr(lse), _stream(q)))
     return (out, lse) if want_lse else out
 
 

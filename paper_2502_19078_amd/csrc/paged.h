@@ -1,0 +1,157 @@
+// Shared by the sources of the paged cache: where a row lies, what 4 bits stand for, which keys a query sees and what is done to its scores.
+#pragma once
+#include "attention.h"
+
+enum PagedType { PAGED_F32 = CLADA_PAGE_F32, PAGED_BF16 = CLADA_PAGE_BF16, PAGED_4BIT = CLADA_PAGE_MX4 };
+
+// Strides in bytes; those of the scales (4 bits) are in bytes of theirs.
+struct PagedKV {
+    const char *k, *v;
+    const unsigned char *ks, *vs;
+    int64_t sp, sh, sn, ssp, ssh, ssn;
+    const int32_t *table;
+    int64_t table_stride;
+    int pages, shift, max_pages;                             // rows of a page: 2^shift
+};
+
+struct PagedArgs : AttnArgs {
+    PagedKV pg;
+    const int32_t *first, *prefix_lens;
+    const float *slopes;
+    float cap2, cap_in;                                      // cap log2(e), and the factor of q . k in tanh's argument, 2 log2(e) scale / cap; cap2 0: none
+    float inv_cap_scale;                                     // scale / cap
+};
+
+clada_status clada_check_paged(clada_ctx *ctx, const clada_paged_cache *c, const char *what, bool data);
+PagedKV clada_paged_of(const clada_paged_cache *c);
+static inline int32_t paged_dtype(const clada_paged_cache *c) { return c->type == CLADA_PAGE_F32 ? CLADA_F32 : CLADA_BF16; }
+
+#ifdef __HIPCC__
+constexpr int paged_es(PagedType ty) { return ty == PAGED_F32 ? 4 : 2; }      // bytes of a query's value
+constexpr int paged_row_bytes(PagedType ty, int d) { return ty == PAGED_4BIT ? d / 2 : d * paged_es(ty); }
+
+// The page of a sequence's position, or -1.
+__device__ __forceinline__ int paged_page(const PagedKV &pg, int b, int p)
+{
+    const int at = p >> pg.shift;
+    const int page = at < pg.max_pages ? pg.table[b * pg.table_stride + at] : -1;
+    return (unsigned int)page < (unsigned int)pg.pages ? page : -1;
+}
+
+// 2^(byte - 127); NaN for 255 (what the conversions below make of an infinite scale).
+__device__ __forceinline__ float paged_unit(unsigned int byte) { return __uint_as_float(byte << 23); }
+
+// Eight values of 4 bits (a word) as eight bf16.
+__device__ __forceinline__ u32x4 paged_bf16x8(unsigned int codes, float unit)
+{
+    u32x4 v;
+    v[0] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0));
+    v[1] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1));
+    v[2] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2));
+    v[3] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3));
+    return v;
+}
+
+// Keys [begin, end) that query t of sequence b sees, at position pos; all zero for one that sees nothing.
+struct RowSpan { int begin, end, pos; };
+__device__ __forceinline__ RowSpan paged_span(const PagedArgs &a, int b, int t, int len, int qlen)
+{
+    RowSpan s = {0, 0, 0};
+    const int pos = len - qlen + t;
+    if (t >= qlen || pos < 0) return s;
+    s.pos = pos;
+    s.end = pos + 1;
+    if (a.prefix_lens) s.end = min(len, max(s.end, a.prefix_lens[b]));
+    if (a.window) s.begin = max(0, pos - a.window + 1);
+    if (a.first) s.begin = max(s.begin, a.first[(int64_t)b * a.T + t]);
+    if (s.begin >= s.end) s.begin = s.end = 0;
+    return s;
+}
+
+// q . k of a key at `far` positions from its query -> score in log2 units.  slope2: slope log2(e).  cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)) is off by
+// a few 2^-24 of cap; in fp32 calls, whose scores may be small beside it, tanhf is not.
+template <PagedType TY>
+__device__ __forceinline__ float paged_score(const PagedArgs &a, float dot, float slope2, float far)
+{
+    float x;
+    if (a.cap2 == 0.0f) x = dot * a.scale2;
+    else if (TY == PAGED_F32) x = a.cap2 * tanhf(dot * a.inv_cap_scale);
+    else x = fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(dot * a.cap_in)), a.cap2);
+    return a.slopes ? fmaf(-slope2, fabsf(far), x) : x;
+}
+
+__device__ __forceinline__ float paged_slope2(const PagedArgs &a, int hq) { return a.slopes ? a.slopes[hq] * 1.4426950408889634f : 0.0f; }
+
+// Value d of a row: `row` its first byte, `units` its first exponent.
+template <PagedType TY>
+__device__ __forceinline__ float paged_value(const char *row, const unsigned char *units, int d)
+{
+    if constexpr (TY == PAGED_4BIT) {
+        typedef __attribute__((ext_vector_type(2))) float f32x2;
+        const unsigned int both = reinterpret_cast<const unsigned char *>(row)[d >> 1];
+        const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(both, paged_unit(units[d >> 5]), 0);
+        return d & 1 ? v[1] : v[0];
+    } else
+        return attn_value<paged_es(TY)>(row, d);
+}
+
+// One row by one wave, key by key as it sees them: 64 keys' scores at once, a lane each, then their values one after the other, a lane for every 64th
+// dimension.  Keys [k0, k1) of sequence b and key head h, those that the row sees.
+template <PagedType TY>
+__device__ __forceinline__ RowAgain paged_row(const PagedArgs &a, int b, int h, const char *q, const RowSpan &s, float slope2, int k0, int k1)
+{
+    const int lane = threadIdx.x & 63;
+    const PagedKV &pg = a.pg;
+    RowAgain r;
+    r.m = NEG_INF;
+    r.l = 0.0f;
+    for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j) r.o[j] = 0.0f;
+    for (int base = max(k0, s.begin); base < min(k1, s.end); base += 64) {
+        const int key = base + lane;
+        const int page = key < min(k1, s.end) ? paged_page(pg, b, key) : -1;
+        const bool see = page >= 0;
+        const int at = key & ((1 << pg.shift) - 1);
+        const int64_t off = see ? page * pg.sp + h * pg.sh + at * pg.sn : 0;
+        const int64_t soff = see && TY == PAGED_4BIT ? page * pg.ssp + h * pg.ssh + at * pg.ssn : 0;
+        float x = NEG_INF;
+        if (see) {
+            float dot = 0.0f;
+            for (int d = 0; d < a.D; ++d) dot = fmaf(paged_value<TY>(pg.k + off, pg.ks + soff, d), attn_value<paged_es(TY)>(q, d), dot);
+            x = paged_score<TY>(a, dot, slope2, (float)(key - s.pos));
+        }
+        const float mn = fmaxf(r.m, wave_max(x)), f = r.m == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(r.m - mn);
+        const float w = see ? __builtin_amdgcn_exp2f(x - (mn == NEG_INF ? 0.0f : mn)) : 0.0f;
+        r.l = r.l * f + wave_sum(w);
+        for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j)
+            if (r.m != NEG_INF) r.o[j] *= f;
+        r.m = mn;
+        for (unsigned long long left = __ballot(see); left; left &= left - 1) {
+            const int t = __builtin_ctzll(left);
+            const float wt = __shfl(w, t);
+            const int64_t row = __shfl(off, t), srow = __shfl(soff, t);
+            for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j)
+                if (lane + 64 * j < a.D) r.o[j] = fmaf(wt, paged_value<TY>(pg.v + row, pg.vs + srow, lane + 64 * j), r.o[j]);
+        }
+    }
+    return r;
+}
+
+// What a row of a split, or of a call without splits, leaves behind: by a wave that holds it as above.
+template <int ES>
+__device__ __forceinline__ void paged_store_row(const PagedArgs &a, const RowAgain &r, const RowAt &at, int part)
+{
+    const int lane = threadIdx.x & 63;
+    if (a.splits > 1) {
+        if (lane == 0) a.part_ml[at.lse * a.splits + part] = make_float2(r.m, r.l);
+    } else if (a.lse && lane == 0)
+        a.lse[at.lse] = r.l == 0.0f ? NEG_INF : r.m * 0.69314718055994531f + logf(r.l);
+    for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j) {
+        const int d = lane + 64 * j;
+        if (d >= a.D) continue;
+        const float y = r.l == 0.0f ? 0.0f : r.o[j] / r.l;
+        if (a.splits > 1) a.part_o[(at.lse * a.splits + part) * a.D + d] = r.o[j];
+        else if (ES == 2) reinterpret_cast<unsigned short *>(a.out + at.o)[d] = (unsigned short)f32_to_bf16_bits(y);
+        else reinterpret_cast<float *>(a.out + at.o)[d] = y;
+    }
+}
+#endif

@@ -1,0 +1,92 @@
+// clada_paged_attn: attention over a paged cache.
+#include <math.h>
+
+#include "paged.h"
+
+namespace {
+
+// One wave a row.
+template <PagedType TY>
+__global__ void __launch_bounds__(256)
+k_paged_rows(const PagedArgs a)
+{
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)a.B * a.T * a.Hq) return;
+    const int hq = (int)(row % a.Hq);
+    const int64_t bt = row / a.Hq;
+    const int b = (int)(bt / a.T), t = (int)(bt % a.T);
+    int len, qlen;
+    sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
+    const RowSpan s = paged_span(a, b, t, len, qlen);
+    const RowAt at = {b * a.q_sb + t * a.q_st + hq * a.q_sh, b * a.o_sb + t * a.o_st + hq * a.o_sh, row};
+    paged_store_row<paged_es(TY)>(a, paged_row<TY>(a, b, hq / a.G, a.q + at.q, s, paged_slope2(a, hq), s.begin, s.end), at, 0);
+}
+
+}  // namespace
+
+extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, const clada_paged_cache *cache, const int32_t *lens, const int32_t *q_lens,
+                                         int32_t B, int32_t T, int32_t Hq, int32_t max_len, const clada_attn_scores *scores, const clada_heads *out,
+                                         float *lse, void *hip_stream)
+{
+    if (!ctx) return CLADA_ERR_NULL;
+    if (!cache || !lens || !scores) return clada_fail(ctx, CLADA_ERR_NULL, "cache, lens or scores is NULL");
+    clada_status st = clada_check_paged(ctx, cache, "cache", true);
+    if (st != CLADA_OK) return st;
+    if (B < 1 || T < 1 || B > CLADA_ATTN_MAX_BATCH || (int64_t)B * T > CLADA_ATTN_MAX_ROWS)
+        return clada_fail(ctx, CLADA_ERR_SHAPE, "B=%d, T=%d: need B in [1,%d], T >= 1 and B*T <= %d", B, T, CLADA_ATTN_MAX_BATCH, CLADA_ATTN_MAX_ROWS);
+    if (Hq < 1 || Hq > CLADA_ATTN_MAX_HEADS || Hq % cache->heads)
+        return clada_fail(ctx, CLADA_ERR_SHAPE, "%d query heads: need a multiple of the cache's %d in [1,%d]", Hq, cache->heads, CLADA_ATTN_MAX_HEADS);
+    if (cache->batch < B) return clada_fail(ctx, CLADA_ERR_SHAPE, "the cache holds %d sequences, the call has %d", cache->batch, B);
+    if (!isfinite(scores->scale)) return clada_fail(ctx, CLADA_ERR_VALUE, "scale is not finite");
+    if (!(scores->cap >= 0.0f) || !isfinite(scores->cap)) return clada_fail(ctx, CLADA_ERR_VALUE, "cap=%g is negative or not finite", scores->cap);
+    if (scores->window < 0 || max_len < 0) return clada_fail(ctx, CLADA_ERR_VALUE, "window=%d, max_len=%d: negative", scores->window, max_len);
+    if (((uintptr_t)lens | (uintptr_t)q_lens | (uintptr_t)lse | (uintptr_t)scores->slopes | (uintptr_t)scores->prefix_lens | (uintptr_t)scores->first) & 3u)
+        return clada_fail(ctx, CLADA_ERR_ALIGN, "lens, q_lens, lse, slopes, prefix_lens and first must be 4-byte aligned");
+    const int32_t dtype = paged_dtype(cache);
+    if ((st = clada_check_heads(ctx, q, dtype, "q")) != CLADA_OK) return st;
+    if ((st = clada_check_out(ctx, out, dtype, B, T, Hq, cache->d, "out")) != CLADA_OK) return st;
+    if (ctx->ws_bytes == 0) return clada_fail(ctx, CLADA_ERR_WORKSPACE, "context has no device");
+
+    const int64_t es = (int64_t)dtype_size(dtype);
+    PagedArgs a = {};
+    a.q = (const char *)q->data;
+    a.q_sb = q->stride_b * es;
+    a.q_st = q->stride_t * es;
+    a.q_sh = q->stride_h * es;
+    a.out = (char *)out->data;
+    a.o_sb = out->stride_b * es;
+    a.o_st = out->stride_t * es;
+    a.o_sh = out->stride_h * es;
+    a.lse = lse;
+    a.lens = lens;
+    a.q_lens = q_lens;
+    a.B = B;
+    a.T = T;
+    a.Hq = Hq;
+    a.Hkv = cache->heads;
+    a.G = Hq / cache->heads;
+    a.D = cache->d;
+    a.pg = clada_paged_of(cache);
+    a.kv.capacity = cache->max_pages * cache->page_size;     // what lens is cut to
+    if (max_len && max_len < a.kv.capacity) a.kv.capacity = max_len;
+    a.window = scores->window >= a.kv.capacity ? 0 : scores->window;       // (as wide as the sequences: everything)
+    a.first = scores->first;
+    a.prefix_lens = scores->prefix_lens;
+    a.slopes = scores->slopes;
+    const double log2e = 1.4426950408889634;
+    a.scale2 = (float)(scores->scale * log2e);
+    if (scores->cap > 0.0f) {
+        a.cap2 = (float)(scores->cap * log2e);
+        a.cap_in = (float)(2.0 * log2e * scores->scale / scores->cap);
+        a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
+    }
+    a.splits = 1;
+    const int64_t rows = (int64_t)B * T * Hq;
+    const dim3 grid((unsigned int)((rows + 3) / 4)), block(256);
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (cache->type == CLADA_PAGE_MX4) hipLaunchKernelGGL(k_paged_rows<PAGED_4BIT>, grid, block, 0, s, a);
+    else if (cache->type == CLADA_PAGE_BF16) hipLaunchKernelGGL(k_paged_rows<PAGED_BF16>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(k_paged_rows<PAGED_F32>, grid, block, 0, s, a);
+    CLADA_CHECK_HIP(ctx, hipGetLastError());
+    return CLADA_OK;
+}
