@@ -32,6 +32,8 @@ struct AttnArgs {
 // Which kernel: tiles of 16 rows, of 128 rows, or a shared prefix in tiles of 128 rows with the sequences' own keys in tiles of 16.  Partial
 // results are joined where there are any.
 enum AttnPath { ATTN_ROWS, ATTN_TILES, ATTN_PREFIX };
+int clada_attn_splits(int64_t units, int64_t keys, int64_t wgs);      // of a tile's keys
+clada_status clada_attn_place(clada_ctx *ctx, AttnArgs &a);          // partial results into the workspace
 hipError_t clada_attn_launch(const AttnArgs &a, int es, AttnPath path, int num_cu, hipStream_t stream);
 
 #ifdef __HIPCC__
@@ -117,6 +119,14 @@ __device__ __forceinline__ void sequence_lens(const AttnArgs &a, int len_b, int 
     len = max(len_b, 0);
     if (a.kv.ring == 0) len = min(len, a.kv.capacity);
     qlen = min(max(qlen_b, 0), a.T);
+}
+
+// Whether a joined row (query t of sequence b, the sum of its weights l) sees nothing; for attention_join.h.
+__device__ __forceinline__ bool joined_none(const AttnArgs &a, int b, int t, float)
+{
+    int len, qlen;
+    sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
+    return a.pre_splits ? a.pre_n + len == 0 : t >= qlen || len - qlen + t < 0;
 }
 
 // A product over a tile gives every row every key of it, and a weight of zero (or the lower half of a weight) times a value that is not finite

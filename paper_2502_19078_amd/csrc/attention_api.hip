@@ -54,17 +54,6 @@ AttnKV kv_of(const clada_kv_cache *c)
     return {(const char *)c->k, (const char *)c->v, c->stride_b * es, c->stride_h * es, c->stride_n * es, c->capacity, c->n_sink, c->ring};
 }
 
-// Splits of `keys` keys for `units` tiles, so that the launch has about `wgs` workgroups; no split under 128 keys (one step of the few-row kernel's
-// waves; two tiles).  One workgroup for all keys of a short sequence costs more than the launch that joins splits (513 keys of one
-// head of 256 values: 26 us against 15).
-int splits_for(int64_t units, int64_t keys, int64_t wgs)
-{
-    const int64_t want = (wgs + units - 1) / units, most = (keys + 127) / 128;
-    int64_t s = want < most ? want : most;
-    if (s > MAX_SPLITS) s = MAX_SPLITS;
-    return s < 1 ? 1 : (int)s;
-}
-
 clada_status check_call(clada_ctx *ctx, const clada_kv_cache *cache, int32_t B, int32_t T, int32_t Hq, float scale, const void *lens, const void *q_lens,
                         const float *lse)
 {
@@ -102,8 +91,21 @@ void fill(AttnArgs &a, const clada_heads *q, const clada_heads *out, const clada
     a.scale2 = (float)((double)scale * 1.4426950408889634);
 }
 
+}  // namespace
+
+// Splits of `keys` keys for `units` tiles, so that the launch has about `wgs` workgroups; no split under 128 keys (one step of the few-row kernel's
+// waves; two tiles).  One workgroup for all keys of a short sequence costs more than the launch that joins splits (513 keys of one
+// head of 256 values: 26 us against 15).
+int clada_attn_splits(int64_t units, int64_t keys, int64_t wgs)
+{
+    const int64_t want = (wgs + units - 1) / units, most = (keys + 127) / 128;
+    int64_t s = want < most ? want : most;
+    if (s > MAX_SPLITS) s = MAX_SPLITS;
+    return s < 1 ? 1 : (int)s;
+}
+
 // Partial results into the workspace.
-clada_status place_parts(clada_ctx *ctx, AttnArgs &a)
+clada_status clada_attn_place(clada_ctx *ctx, AttnArgs &a)
 {
     const int64_t parts = (int64_t)a.B * a.T * a.Hq * (a.splits + a.pre_splits);
     const size_t need = part_bytes(parts, a.D);
@@ -113,8 +115,6 @@ clada_status place_parts(clada_ctx *ctx, AttnArgs &a)
     a.part_o = (float *)(ctx->ws + CLADA_WS_HEADER + align_up((size_t)parts * 8, 256));
     return CLADA_OK;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -169,8 +169,8 @@ clada_status clada_window_attn(clada_ctx *ctx, const clada_heads *q, const clada
     }
     // Few rows: one workgroup a compute unit streams heads of 128 values and more as fast as two, with half the partial results (8 sequences of 8192
     // rows, 8 key heads of 128 values: 54.8 against 57 us); narrower ones it does not (64 values: 37.8 against 33).  Tiles take two.
-    a.splits = splits_for(units, keys, path == ATTN_ROWS && cache->d >= 128 ? ctx->num_cu : 2 * ctx->num_cu);
-    if (a.splits > 1 && (st = place_parts(ctx, a)) != CLADA_OK) return st;
+    a.splits = clada_attn_splits(units, keys, path == ATTN_ROWS && cache->d >= 128 ? ctx->num_cu : 2 * ctx->num_cu);
+    if (a.splits > 1 && (st = clada_attn_place(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, ctx->num_cu, (hipStream_t)hip_stream));
     return CLADA_OK;
 }
@@ -205,9 +205,9 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
     a.own_tiles = (a.G + 15) / 16;
     // One workgroup a compute unit for the prefix and one for the sequences' own keys: 16 sequences behind 8192 rows 20.2 us, with two each 27.2
     // (48 behind 4095: 38.2 and 44).
-    a.pre_splits = splits_for((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
-    a.splits = splits_for((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
-    if ((st = place_parts(ctx, a)) != CLADA_OK) return st;
+    a.pre_splits = clada_attn_splits((int64_t)a.Hkv * a.pre_tiles, prefix_len, ctx->num_cu);
+    a.splits = clada_attn_splits((int64_t)B * a.Hkv * a.own_tiles, cache->capacity, ctx->num_cu);
+    if ((st = clada_attn_place(ctx, a)) != CLADA_OK) return st;
     CLADA_CHECK_HIP(ctx, clada_attn_launch(a, es, path, ctx->num_cu, (hipStream_t)hip_stream));
     return CLADA_OK;
 }

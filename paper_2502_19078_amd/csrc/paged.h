@@ -22,6 +22,9 @@ struct PagedArgs : AttnArgs {
     float inv_cap_scale;                                     // scale / cap
 };
 
+hipError_t clada_paged_launch_f32(const PagedArgs &a, AttnPath path, int num_cu, hipStream_t stream);
+hipError_t clada_paged_launch_bf16(const PagedArgs &a, AttnPath path, int num_cu, hipStream_t stream);
+hipError_t clada_paged_launch_mx4(const PagedArgs &a, AttnPath path, int num_cu, hipStream_t stream);
 clada_status clada_check_paged(clada_ctx *ctx, const clada_paged_cache *c, const char *what, bool data);
 PagedKV clada_paged_of(const clada_paged_cache *c);
 static inline int32_t paged_dtype(const clada_paged_cache *c) { return c->type == CLADA_PAGE_F32 ? CLADA_F32 : CLADA_BF16; }
@@ -71,13 +74,37 @@ __device__ __forceinline__ RowSpan paged_span(const PagedArgs &a, int b, int t, 
 // q . k of a key at `far` positions from its query -> score in log2 units.  slope2: slope log2(e).  cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)) is off by
 // a few 2^-24 of cap; in fp32 calls, whose scores may be small beside it, tanhf is not.
 template <PagedType TY>
+__device__ __forceinline__ float paged_capped(const PagedArgs &a, float dot)
+{
+    if (TY == PAGED_F32) return a.cap2 * tanhf(dot * a.inv_cap_scale);
+    return fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(dot * a.cap_in)), a.cap2);
+}
+template <PagedType TY>
 __device__ __forceinline__ float paged_score(const PagedArgs &a, float dot, float slope2, float far)
 {
-    float x;
-    if (a.cap2 == 0.0f) x = dot * a.scale2;
-    else if (TY == PAGED_F32) x = a.cap2 * tanhf(dot * a.inv_cap_scale);
-    else x = fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(dot * a.cap_in)), a.cap2);
+    const float x = a.cap2 == 0.0f ? dot * a.scale2 : paged_capped<TY>(a, dot);
     return a.slopes ? fmaf(-slope2, fabsf(far), x) : x;
+}
+
+// The same for a lane's scores s[k][e], e < N, of keys `far` + at(k, e) from their query.
+template <PagedType TY, int N, class V, int K, class At>
+__device__ __forceinline__ void paged_scores(const PagedArgs &a, V (&s)[K], float slope2, float far, At &&at)
+{
+    if (a.cap2 == 0.0f) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[k] *= a.scale2;
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < N; ++e) s[k][e] = paged_capped<TY>(a, s[k][e]);
+    }
+    if (a.slopes) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < N; ++e) s[k][e] = fmaf(-slope2, fabsf(far + (float)at(k, e)), s[k][e]);
+    }
 }
 
 __device__ __forceinline__ float paged_slope2(const PagedArgs &a, int hq) { return a.slopes ? a.slopes[hq] * 1.4426950408889634f : 0.0f; }
@@ -154,4 +181,6 @@ __device__ __forceinline__ void paged_store_row(const PagedArgs &a, const RowAga
         else reinterpret_cast<float *>(a.out + at.o)[d] = y;
     }
 }
+// For attention_join.h: a row whose weights sum up to nothing saw no key, or only scores of -inf.
+__device__ __forceinline__ bool joined_none(const PagedArgs &, int, int, float l) { return l == 0.0f; }
 #endif

@@ -16,6 +16,7 @@ clada_status clada_check_paged(clada_ctx *ctx, const clada_paged_cache *c, const
         (int64_t)c->max_pages * c->page_size > CLADA_ATTN_MAX_CAPACITY)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: %d pages of %d rows, %d heads, a table of %d x %d", what, c->pages, c->page_size, c->heads, c->batch, c->max_pages);
     if (c->stride_p < 0 || c->stride_h < 0 || c->stride_n < 0 || c->table_stride < 0) return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: a stride is negative", what);
+    if (c->stride_n > (INT64_C(1) << 26)) return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: rows of a page lie %lld values apart", what, (long long)c->stride_n);
     const int64_t step = c->type == CLADA_PAGE_F32 ? 4 : four ? 32 : 8;
     if (c->stride_p % step || c->stride_h % step || c->stride_n % step || (data && (!aligned16(c->k) || !aligned16(c->v) || ((uintptr_t)c->table & 3u))))
         return clada_fail(ctx, CLADA_ERR_ALIGN, "%s: pointers and strides must be multiples of 16 bytes, the table 4-byte aligned", what);

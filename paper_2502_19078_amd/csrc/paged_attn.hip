@@ -1,28 +1,7 @@
-// clada_paged_attn: attention over a paged cache.
+// clada_paged_attn: what it accepts, and how a call is cut into workgroups.
 #include <math.h>
 
 #include "paged.h"
-
-namespace {
-
-// One wave a row.
-template <PagedType TY>
-__global__ void __launch_bounds__(256)
-k_paged_rows(const PagedArgs a)
-{
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)a.B * a.T * a.Hq) return;
-    const int hq = (int)(row % a.Hq);
-    const int64_t bt = row / a.Hq;
-    const int b = (int)(bt / a.T), t = (int)(bt % a.T);
-    int len, qlen;
-    sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
-    const RowSpan s = paged_span(a, b, t, len, qlen);
-    const RowAt at = {b * a.q_sb + t * a.q_st + hq * a.q_sh, b * a.o_sb + t * a.o_st + hq * a.o_sh, row};
-    paged_store_row<paged_es(TY)>(a, paged_row<TY>(a, b, hq / a.G, a.q + at.q, s, paged_slope2(a, hq), s.begin, s.end), at, 0);
-}
-
-}  // namespace
 
 extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, const clada_paged_cache *cache, const int32_t *lens, const int32_t *q_lens,
                                          int32_t B, int32_t T, int32_t Hq, int32_t max_len, const clada_attn_scores *scores, const clada_heads *out,
@@ -80,13 +59,18 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
         a.cap_in = (float)(2.0 * log2e * scores->scale / scores->cap);
         a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
     }
-    a.splits = 1;
-    const int64_t rows = (int64_t)B * T * Hq;
-    const dim3 grid((unsigned int)((rows + 3) / 4)), block(256);
-    hipStream_t s = (hipStream_t)hip_stream;
-    if (cache->type == CLADA_PAGE_MX4) hipLaunchKernelGGL(k_paged_rows<PAGED_4BIT>, grid, block, 0, s, a);
-    else if (cache->type == CLADA_PAGE_BF16) hipLaunchKernelGGL(k_paged_rows<PAGED_BF16>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(k_paged_rows<PAGED_F32>, grid, block, 0, s, a);
-    CLADA_CHECK_HIP(ctx, hipGetLastError());
+    const AttnPath path = ATTN_ROWS;
+    const int tile = 16;
+    a.own_tiles = (T * a.G + tile - 1) / tile;
+    const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
+    int64_t keys = a.kv.capacity;                            // what a tile can see at most
+    if (a.window && !a.prefix_lens) {
+        const int64_t seen = (int64_t)a.window + tile / a.G;
+        if (seen < keys) keys = seen;
+    }
+    a.splits = clada_attn_splits(units, keys, 2 * ctx->num_cu);
+    if (a.splits > 1 && (st = clada_attn_place(ctx, a)) != CLADA_OK) return st;
+    const auto launch = cache->type == CLADA_PAGE_MX4 ? clada_paged_launch_mx4 : cache->type == CLADA_PAGE_BF16 ? clada_paged_launch_bf16 : clada_paged_launch_f32;
+    CLADA_CHECK_HIP(ctx, launch(a, path, ctx->num_cu, (hipStream_t)hip_stream));
     return CLADA_OK;
 }

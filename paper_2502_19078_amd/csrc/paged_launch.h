@@ -1,0 +1,50 @@
+// Kernels of clada_paged_attn and their launch for one type of page; each type is compiled in a file of its own.
+#pragma once
+#include "attention_join.h"
+#include "paged_rows.h"
+
+namespace {
+
+template <PagedType TY, int DP, bool FULL>
+__global__ void __launch_bounds__(256, TY != PAGED_F32 || DP <= 128 ? 2 : 1)
+k_paged_rows(const PagedArgs a)
+{
+    __shared__ __align__(16) char lds[PagedRowsShape<TY, DP, FULL>::LDS];
+    paged_rows<TY, DP, FULL>(a, blockIdx.x, lds);
+}
+
+template <PagedType TY, int DP>
+void launch_paged_as(const PagedArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
+{
+    if (TY == PAGED_4BIT || a.D == DP) hipLaunchKernelGGL((k_paged_rows<TY, DP, true>), grid, dim3(256), 0, stream, a);
+    else if constexpr (TY != PAGED_4BIT) hipLaunchKernelGGL((k_paged_rows<TY, DP, false>), grid, dim3(256), 0, stream, a);
+}
+
+template <PagedType TY>
+hipError_t launch_paged(const PagedArgs &a, AttnPath path, int num_cu, hipStream_t stream)
+{
+    const dim3 grid((unsigned int)((int64_t)a.B * a.Hkv * a.own_tiles * a.splits));
+    if constexpr (TY == PAGED_4BIT) {
+        switch (a.D / 32) {
+        case 1: launch_paged_as<TY, 32>(a, path, grid, stream); break;
+        case 2: launch_paged_as<TY, 64>(a, path, grid, stream); break;
+        case 3: launch_paged_as<TY, 96>(a, path, grid, stream); break;
+        case 4: launch_paged_as<TY, 128>(a, path, grid, stream); break;
+        case 5: launch_paged_as<TY, 160>(a, path, grid, stream); break;
+        case 6: launch_paged_as<TY, 192>(a, path, grid, stream); break;
+        case 7: launch_paged_as<TY, 224>(a, path, grid, stream); break;
+        default: launch_paged_as<TY, 256>(a, path, grid, stream);
+        }
+    } else {
+        if (a.D <= 64) launch_paged_as<TY, 64>(a, path, grid, stream);
+        else if (a.D <= 96 && TY == PAGED_BF16) launch_paged_as<TY, TY == PAGED_BF16 ? 96 : 128>(a, path, grid, stream);
+        else if (a.D <= 128) launch_paged_as<TY, 128>(a, path, grid, stream);
+        else launch_paged_as<TY, 256>(a, path, grid, stream);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    launch_join(a, paged_es(TY), num_cu, stream);
+    return hipGetLastError();
+}
+
+}  // namespace

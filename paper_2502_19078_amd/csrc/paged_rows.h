@@ -1,0 +1,422 @@
+// The few-row body of clada_paged_attn: single tokens, and calls of at most 16 rows a key head.
+//
+// For a row r and the keys p that it sees:  o_r = sum_p exp(s_rp - lse_r) v_p,  lse_r = log sum_p exp(s_rp), s as paged_score says.  One pass over
+// the keys with a running maximum and sum per row, in base 2.
+//
+// Bound by the pages' bytes (HBM): a key head's rows are read once for all query heads of its group.  A workgroup takes a tile of 16 rows and
+// one split of their keys; its four waves take steps of 16 to 64 keys in turn, each with a running softmax of its own, so nothing waits
+// inside the loop; the waves' results are joined through LDS, those of the splits by k_attn_join.
+//
+// The range of keys begins at a multiple of 16, so each 16 keys lie in one page: its number is one scalar load, made a step ahead of the rows'
+// loads, and the rows have one base.
+//
+// Scores are formed transposed, S^T = K Q^T: a lane then holds scores of one row only, keys 4 (lane / 16) + i of each 16, and the same
+// registers are the operand of O^T = V^T P^T when its keys are counted in that order.  K goes from memory into the operand registers as it
+// lies; 16-bit V goes through LDS, where ds_read_tr16 turns it; fp32 V needs no turning.  The weights enter the second product as two bf16, 16
+// bits.  4 bits: a lane group holds a quarter of a row, its codes become bf16 under their power of two in one instruction for two (exact),
+// K in registers in the order in which the query is taken too, V on its way into LDS.
+#pragma once
+#include "paged.h"
+
+namespace {
+
+// DP: D rounded up to the products' tiles (4 bits: D itself); FULL: D == DP.  KB: 16-key blocks of a step of a wave.
+template <PagedType TY, int DP, bool FULL>
+struct PagedRowsShape {
+    static constexpr int KB = TY == PAGED_F32 ? 1 : TY == PAGED_4BIT ? (DP <= 128 ? 4 : 2) : DP == 256 || (DP == 96 && FULL) ? 1 : 2;
+    static constexpr int KS = 16 * KB;
+    static constexpr int DV = (DP + 15) / 16 * 16;
+    static constexpr int PITCH = DV * 2 + 32;                // V in LDS
+    static constexpr int V_LDS = TY == PAGED_F32 ? 0 : 4 * KS * PITCH, J_LDS = DP * 256 + 512 + 16;     // of the join: outputs and maxima of four waves
+    static constexpr int LDS = V_LDS > J_LDS ? V_LDS : J_LDS;
+};
+
+typedef const __attribute__((address_space(4))) int32_t *scalar_i32;         // read by scalar loads
+
+template <int N> struct Words;
+template <> struct Words<1> { typedef unsigned int type; };
+#define CLADA_WORDS(N) template <> struct Words<N> { typedef __attribute__((ext_vector_type(N), aligned(4))) unsigned int type; };
+CLADA_WORDS(2) CLADA_WORDS(3) CLADA_WORDS(4) CLADA_WORDS(5) CLADA_WORDS(6) CLADA_WORDS(7) CLADA_WORDS(8)
+#undef CLADA_WORDS
+
+template <PagedType TY, int DP, bool FULL>
+__device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, char *lds)
+{
+    using S = PagedRowsShape<TY, DP, FULL>;
+    constexpr int ES = paged_es(TY);
+    constexpr bool FOUR = TY == PAGED_4BIT;
+    constexpr int KB = S::KB, KS = S::KS, PITCH = S::PITCH;
+    constexpr int NW = DP / 32;                              // 4 bits: words of a quarter of a row; also its chunks of 8 values
+    constexpr int CH = FOUR ? NW : DP * ES / 64;             // operand chunks of a row: 16 bytes of every lane group each
+    constexpr int DB = DP / 16;                              // tiles of 16 output dimensions
+    constexpr int CPR = DP * ES / 16;                        // 16-byte chunks of a row of bf16 or fp32
+    constexpr int VL = FOUR ? 1 : KS * CPR / 64;             // 16-byte loads of V a lane and step
+    constexpr int NU = NW == 7 ? 3 : NW == 1 || NW == 2 || NW == 4 ? 1 : 2;     // blocks of 32 values that a quarter of a row touches, at most
+    static_assert(ES == 2 || DP % 64 == 0, "whole loads of V");
+    static_assert(DP % 16 == 0, "whole tiles");
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g = lane >> 4;
+    const int Dd = FULL ? DP : a.D;
+    const PagedKV &pg = a.pg;
+
+    int id = block;
+    const int split = id % a.splits;
+    id /= a.splits;
+    const int tile = id % a.own_tiles;
+    id /= a.own_tiles;
+    const int h = id % a.Hkv, b = id / a.Hkv;
+    const int rows = a.T * a.G, r0 = tile * 16;
+
+    // this lane's row: its query as the second operand.  (Loaded ahead of the lengths, which the keys wait for.)
+    const int len_b = a.lens[b], qlen_b = a.q_lens ? a.q_lens[b] : a.T;
+    const int row = min(r0 + n16, rows - 1), token = a.T == 1 ? 0 : row / a.G;
+    const RowAt at = row_at(a, false, b, h, row, token);
+    u32x4 qf[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int off = FOUR ? g * (DP / 2) + 16 * c : 64 * c + 16 * g;
+        const bool in = FULL || off < Dd * ES;
+        qf[c] = *reinterpret_cast<const u32x4 *>(a.q + at.q + (in ? off : 0));
+        if (!in) qf[c] = u32x4{0, 0, 0, 0};
+    }
+    int len, qlen;
+    sequence_lens(a, len_b, qlen_b, len, qlen);
+    const RowSpan span = paged_span(a, b, token, len, qlen);
+    const float slope2 = paged_slope2(a, h * a.G + row - token * a.G);
+    // keys that any row sees, and those that all see
+    int any0 = span.begin < span.end ? span.begin : INT32_MAX, any1 = span.end, all0 = span.begin, all1 = span.end;
+    if (a.T > 1) {
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) {
+            any0 = min(any0, __shfl_xor(any0, o));
+            any1 = max(any1, __shfl_xor(any1, o));
+            all0 = max(all0, __shfl_xor(all0, o));
+            all1 = min(all1, __shfl_xor(all1, o));
+        }
+    }
+    any0 = __builtin_amdgcn_readfirstlane(any0);
+    any1 = __builtin_amdgcn_readfirstlane(any1);
+    all0 = __builtin_amdgcn_readfirstlane(all0);
+    all1 = __builtin_amdgcn_readfirstlane(all1);
+    const int begin = any1 > 0 ? any0 & ~15 : 0, n = any1 - begin;
+    int chunk = (n + a.splits - 1) / a.splits;
+    chunk = (chunk + KS - 1) / KS * KS;
+    const int64_t from = (int64_t)split * chunk;
+    const int k0 = from < n ? begin + (int)from : any1, k1 = min(k0 + min(chunk, n), any1);
+    const int last16 = k1 > k0 ? (k1 - 1) & ~15 : 0;
+
+    const char *kp = pg.k + h * pg.sh, *vp = pg.v + h * pg.sh;
+    const unsigned char *ksp = pg.ks + h * pg.ssh, *vsp = pg.vs + h * pg.ssh;
+    const scalar_i32 table = (scalar_i32)(uintptr_t)(pg.table + b * pg.table_stride);
+    char *my_v = lds + wave * KS * PITCH;
+
+    f32x4 o[DB];
+    float m = NEG_INF, l = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = f32x4{0, 0, 0, 0};
+
+    // The step's pages, and rows on their way.  A page that is not there is read as page 0 (and not used).
+    int page[KB];
+    int there = 0, there_next = 0;                           // a bit for every block that has a page: of the rows loaded last, and of the pages
+    auto look = [&](int i) {
+        there_next = 0;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int e = table[min(i + 16 * kb, last16) >> pg.shift];
+            const bool ok = (unsigned int)e < (unsigned int)pg.pages;
+            page[kb] = ok ? e : 0;
+            there_next |= ok ? 1 << kb : 0;
+        }
+    };
+    u32x4 kf[FOUR ? 1 : KB][CH], vf[VL];
+    typename Words<NW>::type kc[FOUR ? KB : 1], vc[FOUR ? KB : 1];
+    unsigned char ku[FOUR ? KB : 1][NU], vu[FOUR ? KB : 1][NU];
+    const unsigned int lane_row = (unsigned int)n16 * (unsigned int)pg.sn;
+    const int unit0 = g * NW >> 2;                           // first block of this lane's quarter
+    auto block_at = [&](int i, int kb) { return (int64_t)page[kb] * pg.sp + (int64_t)(min(i + 16 * kb, last16) & ((1 << pg.shift) - 1)) * pg.sn; };
+    auto load_k = [&](int i) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const char *p = kp + block_at(i, kb);
+            if constexpr (FOUR) {
+                kc[kb] = *reinterpret_cast<const typename Words<NW>::type *>(p + (lane_row + (unsigned int)(g * (DP / 8))));
+                const unsigned char *u = ksp + (int64_t)page[kb] * pg.ssp + (int64_t)(min(i + 16 * kb, last16) & ((1 << pg.shift) - 1)) * pg.ssn;
+#pragma unroll
+                for (int j = 0; j < NU; ++j) ku[kb][j] = u[(unsigned int)n16 * (unsigned int)pg.ssn + (unsigned int)min(unit0 + j, NW - 1)];
+            } else
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const int off = 64 * c + 16 * g;
+                    const bool in = FULL || off < Dd * ES;
+                    kf[kb][c] = *reinterpret_cast<const u32x4 *>(p + (lane_row + (unsigned int)(in ? off : 0)));
+                    if (!in) kf[kb][c] = u32x4{0, 0, 0, 0};
+                }
+        }
+    };
+    auto load_v = [&](int i) {
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                vc[kb] = *reinterpret_cast<const typename Words<NW>::type *>(vp + block_at(i, kb) + (lane_row + (unsigned int)(g * (DP / 8))));
+                const unsigned char *u = vsp + (int64_t)page[kb] * pg.ssp + (int64_t)(min(i + 16 * kb, last16) & ((1 << pg.shift) - 1)) * pg.ssn;
+#pragma unroll
+                for (int j = 0; j < NU; ++j) vu[kb][j] = u[(unsigned int)n16 * (unsigned int)pg.ssn + (unsigned int)min(unit0 + j, NW - 1)];
+            }
+        } else
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {                   // bf16: chunks in order of the rows, for LDS; fp32: key 4 g + j % 4, 64 values a load
+                constexpr int PER = 16 * CPR / 64;           // loads of a block
+                const int kb = ES == 2 ? j / PER : 0, x = ES == 2 ? lane + 64 * (j % PER) : 0;
+                const int key = ES == 2 ? x / CPR : 4 * g + j % 4, col = ES == 2 ? x % CPR : 16 * (j / 4) + n16;
+                const bool in = FULL || col * 16 < Dd * ES;
+                vf[j] = *reinterpret_cast<const u32x4 *>(vp + block_at(i, kb) + ((unsigned int)key * (unsigned int)pg.sn + (unsigned int)(in ? col * 16 : 0)));
+                if (!in) vf[j] = u32x4{0, 0, 0, 0};
+            }
+    };
+    // Rows of V that no row sees may hold anything: zeros for them.
+    auto clean_v = [&](int i) {
+        auto dead = [&](int kb, int key) { return !(there >> kb & 1) || i + 16 * kb + key < any0 || i + 16 * kb + key >= any1; };
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                if (dead(kb, n16)) {
+                    vc[kb] = 0;
+#pragma unroll
+                    for (int j = 0; j < NU; ++j) vu[kb][j] = 127;
+                }
+        } else
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {
+                constexpr int PER = 16 * CPR / 64;
+                const int kb = ES == 2 ? j / PER : 0, key = ES == 2 ? (lane + 64 * (j % PER)) / CPR : 4 * g + j % 4;
+                if (dead(kb, key)) vf[j] = u32x4{0, 0, 0, 0};
+            }
+    };
+    auto unit_of = [&](const unsigned char (&u)[NU], int c) {     // of word c
+        const int j = NU == 1 ? 0 : NW == 8 ? c >> 2 : ((g * NW + c) >> 2) - unit0;
+        unsigned int v = u[0];
+#pragma unroll
+        for (int x = 1; x < NU; ++x) v = j == x ? u[x] : v;
+        return paged_unit(v);
+    };
+    auto word = [](const typename Words<NW>::type &w, int c) {
+        if constexpr (NW == 1) return w;
+        else return w[c];
+    };
+
+    int i = k0 + wave * KS;
+    if (i < k1) {
+        look(i);
+        load_k(i);
+        load_v(i);
+        there = there_next;
+        look(i + 4 * KS);
+    }
+    for (; i < k1; i += 4 * KS) {
+        const bool edge = i < all0 || i + KS > all1 || i + KS > k1 || there != (1 << KB) - 1;
+        // scores of KS keys: lane holds keys 16 kb + 4 g + e of its row
+        f32x4 s[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            s[kb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                if constexpr (TY == PAGED_F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned int ka = kf[kb][c][e], qb = qf[c][e];
+                        s[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(ka), __uint_as_float(qb), s[kb], 0, 0, 0);
+                    }
+                } else {
+                    u32x4 k;
+                    if constexpr (FOUR) k = paged_bf16x8(word(kc[kb], c), unit_of(ku[kb], c));
+                    else k = kf[kb][c];
+                    s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[c]), s[kb], 0, 0, 0);
+                }
+            }
+        }
+        if (edge) clean_v(i);
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int c = 0; c < NW; ++c)
+                    *reinterpret_cast<u32x4 *>(my_v + (16 * kb + n16) * PITCH + g * (DP / 2) + 16 * c) = paged_bf16x8(word(vc[kb], c), unit_of(vu[kb], c));
+        } else if constexpr (ES == 2) {
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {
+                const int x = lane + 64 * j;
+                *reinterpret_cast<u32x4 *>(my_v + x / CPR * PITCH + x % CPR * 16) = vf[j];
+            }
+        }
+        const int next = i + 4 * KS, had = there;
+        if (next < k1) {
+            load_k(next);
+            if (ES == 2) {                                   // (in LDS by now)
+                load_v(next);
+                there = there_next;
+                look(next + 4 * KS);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+
+        paged_scores<TY, 4>(a, s, slope2, (float)(i + 4 * g - span.pos), [](int kb, int e) { return 16 * kb + e; });
+        if (edge) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = i + 16 * kb + 4 * g + e;
+                    if (!((had >> kb & 1) && key < k1 && key >= span.begin && key < span.end)) s[kb][e] = NEG_INF;
+                }
+        }
+        float top = NEG_INF;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, s[kb][e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m + 8.0f)) {                         // (weights up to 2^8 lose nothing)
+            const float mn = top > m + 8.0f ? top : m;
+            const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] *= f;
+        }
+        const float base = m == NEG_INF ? 0.0f : m;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(s[kb][e] - base);
+                s[kb][e] = p;
+                l += p;
+            }
+
+        if constexpr (ES == 2) {
+#pragma unroll
+            for (int k2 = 0; k2 < (KB + 1) / 2; ++k2) {      // 32 keys a product (or 16)
+                u32x4 hi = {}, lo = {};
+#pragma unroll
+                for (int w = 0; w < (KB == 1 ? 2 : 4); ++w) {
+                    const float p0 = s[2 * k2 + (w >> 1)][2 * (w & 1)], p1 = s[2 * k2 + (w >> 1)][2 * (w & 1) + 1];
+                    const unsigned int u = pack_bf16(p0, p1);
+                    hi[w] = u;
+                    lo[w] = pack_bf16(p0 - __uint_as_float(u << 16), p1 - __uint_as_float(u & 0xffff0000u));
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const char *src = my_v + (32 * k2 + 4 * g + (n16 >> 2)) * PITCH + d * 32 + (n16 & 3) * 8;
+                    if constexpr (KB == 1) {
+                        const s16x4 vt = __builtin_bit_cast(s16x4, read_tr16(src));
+                        o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, make_uint2(hi[0], hi[1])), o[d], 0, 0, 0);
+                        o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, make_uint2(lo[0], lo[1])), o[d], 0, 0, 0);
+                    } else {
+                        const uint2 u0 = read_tr16(src), u1 = read_tr16(src + 16 * PITCH);
+                        const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{u0.x, u0.y, u1.x, u1.y});
+                        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, hi), o[d], 0, 0, 0);
+                        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, lo), o[d], 0, 0, 0);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VL; ++j)                     // keys 4 g + j % 4, dimensions 64 (j / 4) + 4 n16 + e
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned int vv = vf[j][e];
+                    f32x4 &to = o[(j / 4 * 4 + e) % DB];
+                    to = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vv), s[0][j % 4], to, 0, 0, 0);
+                }
+            if (next < k1) {
+                load_v(next);
+                there = there_next;
+                look(next + 4 * KS);
+            }
+        }
+    }
+
+    // The waves' results side by side in LDS; then every wave joins a part of each row's outputs: v[x] are the four from dim(x) on.
+    constexpr int OUT = (DB + 3) / 4;
+    auto dim = [&](int x) { return ES == 2 ? 16 * (wave + 4 * x) + 4 * g : 64 * x + 16 * g + 4 * wave; };
+    float2 *s_ml = reinterpret_cast<float2 *>(lds + DP * 256);
+    unsigned int *s_again = reinterpret_cast<unsigned int *>(lds + DP * 256 + 512);
+    f32x4 v[OUT];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DB; ++d) reinterpret_cast<f32x4 *>(lds)[(wave * DB + d) * 64 + lane] = o[d];
+    if (g == 0) s_ml[wave * 16 + n16] = make_float2(m, l);
+    if (threadIdx.x == 0) *s_again = 0;
+    __syncthreads();
+    float2 ml[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) ml[w] = s_ml[w * 16 + n16];
+    m = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+    l = 0.0f;
+#pragma unroll
+    for (int x = 0; x < OUT; ++x) v[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = ml[w].x == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(ml[w].x - m);
+        l += ml[w].y * f;
+#pragma unroll
+        for (int x = 0; x < OUT; ++x) {
+            if (ES == 2) {
+                if (DB % 4 == 0 || wave + 4 * x < DB) v[x] += reinterpret_cast<const f32x4 *>(lds)[(w * DB + wave + 4 * x) * 64 + lane] * f;
+            } else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[x][e] += reinterpret_cast<const float *>(lds)[((w * DB + 4 * x + e) * 64 + lane) * 4 + wave] * f;
+        }
+    }
+    bool fine = l < INFINITY;
+#pragma unroll
+    for (int x = 0; x < OUT; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) fine = fine && fabsf(v[x][e]) < INFINITY;
+    unsigned long long odd = __ballot(!fine && !(l != l) && r0 + n16 < rows);
+    if (odd) {
+        odd |= odd >> 32;
+        if (lane == 0) atomicOr(s_again, (unsigned int)((odd | odd >> 16) & 0xffff));
+    }
+    __syncthreads();
+    const unsigned int again = __builtin_amdgcn_readfirstlane(*s_again);
+    if (again) {
+        for (int t = wave; t < 16; t += 4) {
+            if (!(again >> t & 1)) continue;
+            const int i2 = (r0 + t) / a.G;
+            const RowAt to = row_at(a, false, b, h, r0 + t, i2);
+            paged_store_row<ES>(a, paged_row<TY>(a, b, h, a.q + to.q, paged_span(a, b, i2, len, qlen), paged_slope2(a, h * a.G + r0 + t - i2 * a.G), k0, k1), to, split);
+        }
+    }
+
+    if (r0 + n16 >= rows || (again >> n16 & 1)) return;
+    if (a.splits > 1) {
+        const int64_t part = at.lse * a.splits + split;
+        if (g == 0 && wave == 0) a.part_ml[part] = make_float2(m, l);
+        if (k0 >= k1) return;                                // nothing to read for this split
+        float *to = a.part_o + part * Dd;
+#pragma unroll
+        for (int x = 0; x < OUT; ++x)
+            if (dim(x) < Dd) *reinterpret_cast<f32x4 *>(to + dim(x)) = v[x];
+        return;
+    }
+    const bool none = l == 0.0f;                             // sees nothing, or only scores of -inf
+    if (a.lse && g == 0 && wave == 0) a.lse[at.lse] = none ? NEG_INF : (m == NEG_INF ? NEG_INF : m * 0.69314718055994531f) + logf(l);
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int x = 0; x < OUT; ++x) {
+        if (dim(x) >= Dd) continue;
+        const f32x4 y = none ? f32x4{0, 0, 0, 0} : v[x] * inv;
+        if (ES == 2)
+            *reinterpret_cast<uint2 *>(a.out + at.o + dim(x) * 2) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+        else
+            *reinterpret_cast<f32x4 *>(a.out + at.o + dim(x) * 4) = y;
+    }
+}
+
+}  // namespace
