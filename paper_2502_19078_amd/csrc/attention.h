@@ -1,5 +1,7 @@
 // Shared by the attention sources of libclada: what the kernels are told about a call, and how rows and keys are counted.
 #pragma once
+#include <utility>
+
 #include "clada_internal.h"
 
 // Keys and values of one kind of row: strides in bytes.
@@ -50,6 +52,20 @@ __device__ __forceinline__ unsigned int pack_bf16(float lo, float hi)      // ro
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     return __builtin_bit_cast(unsigned int, __builtin_convertvector((f32x2{lo, hi}), bf16x2_t));
 }
+
+// Orders the LDS accesses around it; leaves loads from memory in flight.
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// f(0) .. f(N - 1) with the index as a constant.
+template <class F, int... I>
+__device__ __forceinline__ void unrolled_(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F &&f) { unrolled_(f, std::make_integer_sequence<int, N>{}); }
 
 // Where a row's query and output lie.
 struct RowAt { int64_t q, o, lse; };

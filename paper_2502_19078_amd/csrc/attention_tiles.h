@@ -22,25 +22,10 @@
 // the error is 0.00167 in place of 0.0023.
 #pragma once
 #include <type_traits>
-#include <utility>
 
 #include "attention.h"
 
 namespace {
-
-// Orders the LDS accesses around it; leaves loads from memory in flight.
-__device__ __forceinline__ void tile_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
-// f(0) .. f(N - 1) with the index as a constant.
-template <class F, int... I>
-__device__ __forceinline__ void unrolled_(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
-template <int N, class F>
-__device__ __forceinline__ void unrolled(F &&f) { unrolled_(f, std::make_integer_sequence<int, N>{}); }
 
 template <int ES, int DP>
 struct TilesShape {

@@ -90,21 +90,9 @@ __device__ __forceinline__ float paged_score(const PagedArgs &a, float dot, floa
 template <PagedType TY, int N, class V, int K, class At>
 __device__ __forceinline__ void paged_scores(const PagedArgs &a, V (&s)[K], float slope2, float far, At &&at)
 {
-    if (a.cap2 == 0.0f) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) s[k] *= a.scale2;
-    } else {
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < N; ++e) s[k][e] = paged_capped<TY>(a, s[k][e]);
-    }
-    if (a.slopes) {
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < N; ++e) s[k][e] = fmaf(-slope2, fabsf(far + (float)at(k, e)), s[k][e]);
-    }
+    if (a.cap2 == 0.0f) unrolled<K * N>([&](auto x) { s[x / N][x % N] *= a.scale2; });
+    else unrolled<K * N>([&](auto x) { s[x / N][x % N] = paged_capped<TY>(a, s[x / N][x % N]); });
+    if (a.slopes) unrolled<K * N>([&](auto x) { s[x / N][x % N] = fmaf(-slope2, fabsf(far + (float)at(x / N, x % N)), s[x / N][x % N]); });
 }
 
 __device__ __forceinline__ float paged_slope2(const PagedArgs &a, int hq) { return a.slopes ? a.slopes[hq] * 1.4426950408889634f : 0.0f; }

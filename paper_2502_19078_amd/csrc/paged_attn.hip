@@ -59,8 +59,8 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
         a.cap_in = (float)(2.0 * log2e * scores->scale / scores->cap);
         a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
     }
-    const AttnPath path = ATTN_ROWS;
-    const int tile = 16;
+    const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
+    const int tile = path == ATTN_ROWS ? 16 : 128;
     a.own_tiles = (T * a.G + tile - 1) / tile;
     const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
     int64_t keys = a.kv.capacity;                            // what a tile can see at most

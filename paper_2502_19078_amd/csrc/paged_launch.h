@@ -1,7 +1,7 @@
 // Kernels of clada_paged_attn and their launch for one type of page; each type is compiled in a file of its own.
 #pragma once
 #include "attention_join.h"
-#include "paged_rows.h"
+#include "paged_tiles.h"
 
 namespace {
 
@@ -13,11 +13,29 @@ k_paged_rows(const PagedArgs a)
     paged_rows<TY, DP, FULL>(a, blockIdx.x, lds);
 }
 
+template <PagedType TY, int DP, bool FULL, bool MODS>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
+k_paged_tiles(const PagedArgs a)
+{
+    __shared__ __align__(16) char lds[PagedTilesShape<TY, DP>::LDS];
+    paged_tiles<TY, DP, FULL, MODS>(a, blockIdx.x, lds);
+}
+
+template <PagedType TY, int DP, bool FULL>
+void launch_paged_full(const PagedArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
+{
+    if (path == ATTN_TILES) {
+        if (a.cap2 != 0.0f || a.slopes) hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, false>), grid, dim3(256), 0, stream, a);
+    } else if constexpr (TY != PAGED_F32 || DP % 64 == 0)    // (the rows of the fp32 kernels come in 64 values)
+        hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL>), grid, dim3(256), 0, stream, a);
+}
+
 template <PagedType TY, int DP>
 void launch_paged_as(const PagedArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
 {
-    if (TY == PAGED_4BIT || a.D == DP) hipLaunchKernelGGL((k_paged_rows<TY, DP, true>), grid, dim3(256), 0, stream, a);
-    else if constexpr (TY != PAGED_4BIT) hipLaunchKernelGGL((k_paged_rows<TY, DP, false>), grid, dim3(256), 0, stream, a);
+    if (TY == PAGED_4BIT || a.D == DP) launch_paged_full<TY, DP, true>(a, path, grid, stream);
+    else if constexpr (TY != PAGED_4BIT) launch_paged_full<TY, DP, false>(a, path, grid, stream);
 }
 
 template <PagedType TY>
@@ -37,7 +55,7 @@ hipError_t launch_paged(const PagedArgs &a, AttnPath path, int num_cu, hipStream
         }
     } else {
         if (a.D <= 64) launch_paged_as<TY, 64>(a, path, grid, stream);
-        else if (a.D <= 96 && TY == PAGED_BF16) launch_paged_as<TY, TY == PAGED_BF16 ? 96 : 128>(a, path, grid, stream);
+        else if (a.D <= 96 && (TY == PAGED_BF16 || path == ATTN_TILES)) launch_paged_as<TY, 96>(a, path, grid, stream);
         else if (a.D <= 128) launch_paged_as<TY, 128>(a, path, grid, stream);
         else launch_paged_as<TY, 256>(a, path, grid, stream);
     }
