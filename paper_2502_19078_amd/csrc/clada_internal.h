@@ -53,7 +53,9 @@ enum { COOP_EPOCH = 1024, COOP_FAULT = 1088, STACK_EPOCH = 1152,
        COOP_REC = 4096 /* 256 records of 8 bytes */, STACK_REC = 6144 /* 3 x 256 records */,
        STACK_KCNT = 12288 /* 3 x 256 int32 */,
        COOP_APUB = 16384 /* 256*64 tagged words of 8 bytes = 128 KiB */,
-       STACK_APUB = 16384 + 131072 /* 2 x 128 KiB, ends at 400 KiB */ };
+       STACK_APUB = 16384 + 131072 /* 2 x 128 KiB, ends at 400 KiB */,
+       PAGED_ARRIVED = 400 * 1024 /* 4096 int32, ends at 416 KiB */ };
+#define PAGED_MAX_ARRIVED 4096
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

@@ -4,11 +4,12 @@
 
 enum PagedType { PAGED_F32 = CLADA_PAGE_F32, PAGED_BF16 = CLADA_PAGE_BF16, PAGED_4BIT = CLADA_PAGE_MX4 };
 
-// Strides in bytes; those of the scales (4 bits) are in bytes of theirs.
+// Strides in units of 16 bytes.  16 bytes of 4 bits have one byte of scales, so a row's unit is also its first scale's byte.
 struct PagedKV {
     const char *k, *v;
     const unsigned char *ks, *vs;
-    int64_t sp, sh, sn, ssp, ssh, ssn;
+    int64_t sh;                                              // head
+    unsigned int sp, sn;                                     // page, row
     const int32_t *table;
     int64_t table_stride;
     int pages, shift, max_pages;                             // rows of a page: 2^shift
@@ -18,6 +19,8 @@ struct PagedArgs : AttnArgs {
     PagedKV pg;
     const int32_t *first, *prefix_lens;
     const float *slopes;
+    int *arrived;                                            // splits of a tile that are done, 0 between the calls
+    int tile_rows;                                           // rows of a tile: 8, 16 or 128
     float cap2, cap_in;                                      // cap log2(e), and the factor of q . k in tanh's argument, 2 log2(e) scale / cap; cap2 0: none
     float inv_cap_scale;                                     // scale / cap
 };
@@ -41,8 +44,14 @@ __device__ __forceinline__ int paged_page(const PagedKV &pg, int b, int p)
     return (unsigned int)page < (unsigned int)pg.pages ? page : -1;
 }
 
+// Unit of a page's row, heads aside.
+__device__ __forceinline__ int64_t paged_unit_at(const PagedKV &pg, int page, int row)
+{
+    return (int64_t)((unsigned long long)(unsigned int)page * pg.sp + (unsigned long long)(unsigned int)row * pg.sn);
+}
+
 // 2^(byte - 127); NaN for 255 (what the conversions below make of an infinite scale).
-__device__ __forceinline__ float paged_unit(unsigned int byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ float paged_scale(unsigned int byte) { return __uint_as_float(byte << 23); }
 
 // Eight values of 4 bits (a word) as eight bf16.
 __device__ __forceinline__ u32x4 paged_bf16x8(unsigned int codes, float unit)
@@ -104,7 +113,7 @@ __device__ __forceinline__ float paged_value(const char *row, const unsigned cha
     if constexpr (TY == PAGED_4BIT) {
         typedef __attribute__((ext_vector_type(2))) float f32x2;
         const unsigned int both = reinterpret_cast<const unsigned char *>(row)[d >> 1];
-        const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(both, paged_unit(units[d >> 5]), 0);
+        const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(both, paged_scale(units[d >> 5]), 0);
         return d & 1 ? v[1] : v[0];
     } else
         return attn_value<paged_es(TY)>(row, d);
@@ -126,12 +135,11 @@ __device__ __forceinline__ RowAgain paged_row(const PagedArgs &a, int b, int h, 
         const int page = key < min(k1, s.end) ? paged_page(pg, b, key) : -1;
         const bool see = page >= 0;
         const int at = key & ((1 << pg.shift) - 1);
-        const int64_t off = see ? page * pg.sp + h * pg.sh + at * pg.sn : 0;
-        const int64_t soff = see && TY == PAGED_4BIT ? page * pg.ssp + h * pg.ssh + at * pg.ssn : 0;
+        const int64_t unit = see ? paged_unit_at(pg, page, at) + h * pg.sh : 0;
         float x = NEG_INF;
         if (see) {
             float dot = 0.0f;
-            for (int d = 0; d < a.D; ++d) dot = fmaf(paged_value<TY>(pg.k + off, pg.ks + soff, d), attn_value<paged_es(TY)>(q, d), dot);
+            for (int d = 0; d < a.D; ++d) dot = fmaf(paged_value<TY>(pg.k + unit * 16, pg.ks + unit, d), attn_value<paged_es(TY)>(q, d), dot);
             x = paged_score<TY>(a, dot, slope2, (float)(key - s.pos));
         }
         const float mn = fmaxf(r.m, wave_max(x)), f = r.m == NEG_INF ? 0.0f : __builtin_amdgcn_exp2f(r.m - mn);
@@ -143,12 +151,23 @@ __device__ __forceinline__ RowAgain paged_row(const PagedArgs &a, int b, int h, 
         for (unsigned long long left = __ballot(see); left; left &= left - 1) {
             const int t = __builtin_ctzll(left);
             const float wt = __shfl(w, t);
-            const int64_t row = __shfl(off, t), srow = __shfl(soff, t);
+            const int64_t row = __shfl(unit, t);
             for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j)
-                if (lane + 64 * j < a.D) r.o[j] = fmaf(wt, paged_value<TY>(pg.v + row, pg.vs + srow, lane + 64 * j), r.o[j]);
+                if (lane + 64 * j < a.D) r.o[j] = fmaf(wt, paged_value<TY>(pg.v + row * 16, pg.vs + row, lane + 64 * j), r.o[j]);
         }
     }
     return r;
+}
+
+// Partial results go to memory and come from there, past the L2, which the workgroup that joins them need not share: a fence for the whole L2 (tried in
+// every wave) took 100 us of a call.
+__device__ __forceinline__ void store_past(void *to, float2 v)
+{
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(to), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_past(const void *from)
+{
+    return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const unsigned long long *>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
 // What a row of a split, or of a call without splits, leaves behind: by a wave that holds it as above.
@@ -157,14 +176,14 @@ __device__ __forceinline__ void paged_store_row(const PagedArgs &a, const RowAga
 {
     const int lane = threadIdx.x & 63;
     if (a.splits > 1) {
-        if (lane == 0) a.part_ml[at.lse * a.splits + part] = make_float2(r.m, r.l);
+        if (lane == 0) store_past(&a.part_ml[at.lse * a.splits + part], make_float2(r.m, r.l));
     } else if (a.lse && lane == 0)
         a.lse[at.lse] = r.l == 0.0f ? NEG_INF : r.m * 0.69314718055994531f + logf(r.l);
     for (int j = 0; j < CLADA_ATTN_MAX_D / 64; ++j) {
         const int d = lane + 64 * j;
         if (d >= a.D) continue;
         const float y = r.l == 0.0f ? 0.0f : r.o[j] / r.l;
-        if (a.splits > 1) a.part_o[(at.lse * a.splits + part) * a.D + d] = r.o[j];
+        if (a.splits > 1) __hip_atomic_store(&a.part_o[(at.lse * a.splits + part) * a.D + d], r.o[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         else if (ES == 2) reinterpret_cast<unsigned short *>(a.out + at.o)[d] = (unsigned short)f32_to_bf16_bits(y);
         else reinterpret_cast<float *>(a.out + at.o)[d] = y;
     }

@@ -16,7 +16,8 @@ clada_status clada_check_paged(clada_ctx *ctx, const clada_paged_cache *c, const
         (int64_t)c->max_pages * c->page_size > CLADA_ATTN_MAX_CAPACITY)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: %d pages of %d rows, %d heads, a table of %d x %d", what, c->pages, c->page_size, c->heads, c->batch, c->max_pages);
     if (c->stride_p < 0 || c->stride_h < 0 || c->stride_n < 0 || c->table_stride < 0) return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: a stride is negative", what);
-    if (c->stride_n > (INT64_C(1) << 26)) return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: rows of a page lie %lld values apart", what, (long long)c->stride_n);
+    if (c->stride_n > (INT64_C(1) << 26) || c->stride_p > (INT64_C(1) << 33))
+        return clada_fail(ctx, CLADA_ERR_SHAPE, "%s: rows %lld and pages %lld values apart", what, (long long)c->stride_n, (long long)c->stride_p);
     const int64_t step = c->type == CLADA_PAGE_F32 ? 4 : four ? 32 : 8;
     if (c->stride_p % step || c->stride_h % step || c->stride_n % step || (data && (!aligned16(c->k) || !aligned16(c->v) || ((uintptr_t)c->table & 3u))))
         return clada_fail(ctx, CLADA_ERR_ALIGN, "%s: pointers and strides must be multiples of 16 bytes, the table 4-byte aligned", what);
@@ -27,19 +28,14 @@ PagedKV clada_paged_of(const clada_paged_cache *c)
 {
     PagedKV p = {};
     const bool four = c->type == CLADA_PAGE_MX4;
-    auto bytes = [&](int64_t n) { return c->type == CLADA_PAGE_F32 ? n * 4 : four ? n / 2 : n * 2; };
+    auto units = [&](int64_t n) { return c->type == CLADA_PAGE_F32 ? n / 4 : four ? n / 32 : n / 8; };
     p.k = (const char *)c->k;
     p.v = (const char *)c->v;
-    p.sp = bytes(c->stride_p);
-    p.sh = bytes(c->stride_h);
-    p.sn = bytes(c->stride_n);
-    if (four) {
-        p.ks = c->k_scales;
-        p.vs = c->v_scales;
-        p.ssp = c->stride_p / 32;
-        p.ssh = c->stride_h / 32;
-        p.ssn = c->stride_n / 32;
-    }
+    p.sh = units(c->stride_h);
+    p.sp = (unsigned int)units(c->stride_p);
+    p.sn = (unsigned int)units(c->stride_n);
+    p.ks = four ? c->k_scales : nullptr;
+    p.vs = four ? c->v_scales : nullptr;
     p.table = c->table;
     p.table_stride = c->table_stride;
     p.pages = c->pages;
@@ -74,10 +70,11 @@ k_paged_read(const ReadArgs a)
     u32x4 x = {0, 0, 0, 0};
     if (page >= 0) {
         const int at = pos & ((1 << a.pg.shift) - 1);
-        const char *from = (values ? a.pg.v : a.pg.k) + page * a.pg.sp + h * a.pg.sh + at * a.pg.sn;
+        const int64_t unit = paged_unit_at(a.pg, page, at) + h * a.pg.sh;
+        const char *from = (values ? a.pg.v : a.pg.k) + unit * 16;
         if (TY == PAGED_4BIT) {
-            const unsigned char unit = ((values ? a.pg.vs : a.pg.ks) + page * a.pg.ssp + h * a.pg.ssh + at * a.pg.ssn)[c / 4];
-            x = paged_bf16x8(reinterpret_cast<const unsigned int *>(from)[c], paged_unit(unit));
+            const unsigned char scale = (values ? a.pg.vs : a.pg.ks)[unit + c / 4];
+            x = paged_bf16x8(reinterpret_cast<const unsigned int *>(from)[c], paged_scale(scale));
         } else
             x = reinterpret_cast<const u32x4 *>(from)[c];
     }

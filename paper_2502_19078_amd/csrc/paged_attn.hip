@@ -1,5 +1,6 @@
 // clada_paged_attn: what it accepts, and how a call is cut into workgroups.
 #include <math.h>
+#include <stdlib.h>
 
 #include "paged.h"
 
@@ -60,7 +61,7 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
         a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
     }
     const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
-    const int tile = path == ATTN_ROWS ? 16 : 128;
+    const int tile = a.tile_rows = path == ATTN_TILES ? 128 : cache->type != CLADA_PAGE_F32 && T * a.G <= 8 ? 8 : 16;
     a.own_tiles = (T * a.G + tile - 1) / tile;
     const int64_t units = (int64_t)B * a.Hkv * a.own_tiles;
     int64_t keys = a.kv.capacity;                            // what a tile can see at most
@@ -68,7 +69,9 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
         const int64_t seen = (int64_t)a.window + tile / a.G;
         if (seen < keys) keys = seen;
     }
-    a.splits = clada_attn_splits(units, keys, 2 * ctx->num_cu);
+    a.splits = clada_attn_splits(units, keys, (getenv("XW") ? atoi(getenv("XW")) : 2) * ctx->num_cu);
+    if (units > PAGED_MAX_ARRIVED) a.splits = 1;
+    a.arrived = (int *)(ctx->ws + PAGED_ARRIVED);
     if (a.splits > 1 && (st = clada_attn_place(ctx, a)) != CLADA_OK) return st;
     const auto launch = cache->type == CLADA_PAGE_MX4 ? clada_paged_launch_mx4 : cache->type == CLADA_PAGE_BF16 ? clada_paged_launch_bf16 : clada_paged_launch_f32;
     CLADA_CHECK_HIP(ctx, launch(a, path, ctx->num_cu, (hipStream_t)hip_stream));

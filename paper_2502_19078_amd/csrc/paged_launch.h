@@ -5,12 +5,12 @@
 
 namespace {
 
-template <PagedType TY, int DP, bool FULL>
-__global__ void __launch_bounds__(256, TY != PAGED_F32 || DP <= 128 ? 2 : 1)
+template <PagedType TY, int DP, bool FULL, bool EIGHT>
+__global__ void __launch_bounds__((64 * PagedRowsShape<TY, DP, FULL>::WAVES), TY == PAGED_4BIT && DP <= 128 ? 4 : TY != PAGED_F32 || DP <= 128 ? 2 : 1)
 k_paged_rows(const PagedArgs a)
 {
     __shared__ __align__(16) char lds[PagedRowsShape<TY, DP, FULL>::LDS];
-    paged_rows<TY, DP, FULL>(a, blockIdx.x, lds);
+    paged_rows<TY, DP, FULL, EIGHT>(a, blockIdx.x, lds);
 }
 
 template <PagedType TY, int DP, bool FULL, bool MODS>
@@ -27,8 +27,10 @@ void launch_paged_full(const PagedArgs &a, AttnPath path, dim3 grid, hipStream_t
     if (path == ATTN_TILES) {
         if (a.cap2 != 0.0f || a.slopes) hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, true>), grid, dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, false>), grid, dim3(256), 0, stream, a);
-    } else if constexpr (TY != PAGED_F32 || DP % 64 == 0)    // (the rows of the fp32 kernels come in 64 values)
-        hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL>), grid, dim3(256), 0, stream, a);
+    } else if constexpr (TY != PAGED_F32 || DP % 64 == 0) {  // (the rows of the fp32 kernels come in 64 values)
+        if (TY != PAGED_F32 && a.tile_rows == 8) hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, TY != PAGED_F32>), grid, dim3(64 * PagedRowsShape<TY, DP, FULL>::WAVES), 0, stream, a);
+        else hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, false>), grid, dim3(64 * PagedRowsShape<TY, DP, FULL>::WAVES), 0, stream, a);
+    }
 }
 
 template <PagedType TY, int DP>
@@ -60,7 +62,7 @@ hipError_t launch_paged(const PagedArgs &a, AttnPath path, int num_cu, hipStream
         else launch_paged_as<TY, 256>(a, path, grid, stream);
     }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
+    if (e != hipSuccess || a.splits == 1 || path == ATTN_ROWS) return e;      // (rows are joined by the last split's workgroup)
     launch_join(a, paged_es(TY), num_cu, stream);
     return hipGetLastError();
 }

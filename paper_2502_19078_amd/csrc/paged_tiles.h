@@ -104,14 +104,14 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
 
     // Staging.  16 and 32 bits: a wave's rows of a pass lie in one 16-key block, whose page is a scalar; 4 bits: a thread has one row of K and of V.
     // A page that is not there is read as page 0 (and not used).
-    const char *kp = pg.k + h * pg.sh, *vp = pg.v + h * pg.sh;
-    const unsigned char *ksp = pg.ks + h * pg.ssh, *vsp = pg.vs + h * pg.ssh;
+    const char *kp = pg.k + h * pg.sh * 16, *vp = pg.v + h * pg.sh * 16;
+    const unsigned char *ksp = pg.ks + h * pg.sh, *vsp = pg.vs + h * pg.sh;
     const int32_t *table = pg.table + b * pg.table_stride;
     const scalar_i32 table_s = (scalar_i32)(uintptr_t)table;
     const int in_page = (1 << pg.shift) - 1;
     const int first_key = FOUR ? tid / NG : tid / CPR, col = FOUR ? tid % NG : tid % CPR * 16;
     const bool in = FOUR ? first_key < KT : WHOLE || col < Dd * ES;
-    const unsigned int lane_off = FOUR ? 0u : (unsigned int)(lane / CPR) * (unsigned int)pg.sn + (in ? col : 0);
+    const unsigned int lane_off = FOUR ? 0u : (unsigned int)(lane / CPR) * pg.sn * 16 + (in ? col : 0);
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
     unsigned int uk = 127, uv = 127;
     int page[NB], my_page = 0;                               // of the tile that is fetched next
@@ -135,8 +135,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
         if constexpr (FOUR) {
             // (rows past the last block are read as rows of it, and those ahead of the first one as its)
             const int p = first_key < KT ? i + first_key : i, row = max(min(p & ~15, last16), k0) + (p & 15);
-            at_j[0] = my_page * pg.sp + (int64_t)(row & in_page) * pg.sn + (in ? col * 16 : 0);
-            at_u = my_page * pg.ssp + (int64_t)(row & in_page) * pg.ssn + (in ? col : 0);
+            at_u = paged_unit_at(pg, my_page, row & in_page) + (in ? col : 0);
         } else
 #pragma unroll
             for (int j = 0; j < ROWS; ++j) {
@@ -144,17 +143,17 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
                 int pj = page[0];
 #pragma unroll
                 for (int y = 1; y < NB; ++y) pj = x == y ? page[y] : pj;
-                at_j[j] = pj * pg.sp + (int64_t)((max(min(i + 16 * x, last16), k0) & in_page) + first % 16) * pg.sn;
+                at_j[j] = paged_unit_at(pg, pj, (max(min(i + 16 * x, last16), k0) & in_page) + first % 16) * 16;
             }
         there_reg = there_next;
     };
     auto take = [&](int q) {                                 // transfer q of that tile: K, V, K, ..
         if constexpr (FOUR) {
             if (q & 1) {
-                sv[0] = *reinterpret_cast<const u32x4 *>(vp + at_j[0]);
+                sv[0] = *reinterpret_cast<const u32x4 *>(vp + at_u * 16);
                 uv = vsp[at_u];
             } else {
-                sk[0] = *reinterpret_cast<const u32x4 *>(kp + at_j[0]);
+                sk[0] = *reinterpret_cast<const u32x4 *>(kp + at_u * 16);
                 uk = ksp[at_u];
             }
         } else {
@@ -175,7 +174,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
             if (KT * NG < 256 && !in) return;
             const int c = q & 3;
             char *to = lds + ((q & 4 ? put_v : put_k) + buf * BUF) + c * 16;
-            *reinterpret_cast<u32x4 *>(to) = q & 4 ? paged_bf16x8(sv[0][c], paged_unit(uv)) : paged_bf16x8(sk[0][c], paged_unit(uk));
+            *reinterpret_cast<u32x4 *>(to) = q & 4 ? paged_bf16x8(sv[0][c], paged_scale(uv)) : paged_bf16x8(sk[0][c], paged_scale(uk));
         } else {
             const int j = q / 2;
             u32x4 x = q & 1 ? sv[j] : sk[j];
@@ -265,10 +264,10 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
         for (int k = 0; k < KB; ++k)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
-        top = fmaxf(top, __shfl_xor(top, 32));
         if (!MODS) top *= scale2;
         if constexpr (EDGE) {
             if (__any(top > m + 8.0f)) {                     // (weights above 1 lose nothing)
+                top = fmaxf(top, __shfl_xor(top, 32));
                 const float mn = top > m + 8.0f ? top : m;
                 const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
                 m = mn;

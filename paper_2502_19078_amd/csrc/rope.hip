@@ -224,7 +224,7 @@ k_qk_rope(const RopeArgs a)
                     }
                     if (!four.value && mine[k]) *reinterpret_cast<u32x4 *>(dst + hj * dst_h + ch[k] * 16) = pack_row16<ES>(z[k]);
                 }
-                if (four.value) store_4bit(z, dst + hj * dst_h, unit + hj * a.pg.ssh);
+                if (four.value) store_4bit(z, dst + hj * dst_h, unit + hj * a.pg.sh);
             }
         }
     };
@@ -270,7 +270,7 @@ k_qk_rope(const RopeArgs a)
     if (slot < 0) return;
     const int k0 = (slab + a.slabs - a.Hq % a.slabs) % a.slabs, v0 = (slab + a.slabs - (a.Hq + a.Hk) % a.slabs) % a.slabs;
     char *kc = a.kc + home * a.c_s[0] + slot * a.c_s[1], *vc = a.vc + home * a.c_s[0] + slot * a.c_s[1];
-    const int64_t units = INTO == INTO_4BIT ? home * a.pg.ssp + slot * a.pg.ssn : 0;      // of the scales
+    const int64_t units = INTO == INTO_4BIT ? paged_unit_at(a.pg, (int)home, (int)slot) : 0;      // of the scales
     if (k0 < a.Hk) {
         coefficients((const char *)a.kw, u, v);
         turn_heads(std::bool_constant<INTO == INTO_4BIT>{}, a.k + b * a.k_s[0] + t * a.k_s[1], a.k_s[2], kc, a.c_s[2], const_cast<unsigned char *>(a.pg.ks) + units,
@@ -283,7 +283,7 @@ k_qk_rope(const RopeArgs a)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 unpack_row16(mine[k] ? *reinterpret_cast<const u32x4 *>(vs + h * a.v_s[2] + ch[k] * 16) : u32x4{0, 0, 0, 0}, z[k]);
-            store_4bit(z, vc + h * a.c_s[2], const_cast<unsigned char *>(a.pg.vs) + units + h * a.pg.ssh);
+            store_4bit(z, vc + h * a.c_s[2], const_cast<unsigned char *>(a.pg.vs) + units + h * a.pg.sh);
         }
         return;
     }
@@ -410,9 +410,9 @@ clada_status rope_call(clada_ctx *ctx, const clada_rope *rope, const clada_head_
             a.pg = clada_paged_of(paged);
             a.kc = (char *)paged->k;
             a.vc = (char *)paged->v;
-            a.c_s[0] = a.pg.sp;
-            a.c_s[1] = a.pg.sn;
-            a.c_s[2] = a.pg.sh;
+            a.c_s[0] = 16 * (int64_t)a.pg.sp;
+            a.c_s[1] = 16 * (int64_t)a.pg.sn;
+            a.c_s[2] = 16 * a.pg.sh;
         }
     }
     a.positions = positions;
