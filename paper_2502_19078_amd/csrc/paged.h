@@ -20,9 +20,9 @@ struct PagedArgs : AttnArgs {
     const int32_t *first, *prefix_lens;
     const float *slopes;
     int *arrived;                                            // splits of a tile that are done, 0 between the calls
+    int snake;                                               // order of the row tiles (paged_tiles.h)
     int tile_rows;                                           // rows of a tile: 8, 16 or 128
-    float cap2, cap_in;                                      // cap log2(e), and the factor of q . k in tanh's argument, 2 log2(e) scale / cap; cap2 0: none
-    float inv_cap_scale;                                     // scale / cap
+    float cap2, inv_cap_scale;                               // cap log2(e) (0: none), scale / cap
 };
 
 hipError_t clada_paged_launch_f32(const PagedArgs &a, AttnPath path, int num_cu, hipStream_t stream);
@@ -80,18 +80,35 @@ __device__ __forceinline__ RowSpan paged_span(const PagedArgs &a, int b, int t, 
     return s;
 }
 
-// q . k of a key at `far` positions from its query -> score in log2 units.  slope2: slope log2(e).  cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)) is off by
-// a few 2^-24 of cap; in fp32 calls, whose scores may be small beside it, tanhf is not.
-template <PagedType TY>
-__device__ __forceinline__ float paged_capped(const PagedArgs &a, float dot)
+// cap log2(e) tanh(u), u = x / cap.  In 16 and 4 bits: up to |u| = 0.7 an odd polynomial of five terms (least largest error, 1.6 2^-24, found by
+// weighted least squares; seven instructions of a clock each in place of three and two that take four), beyond it 1 - 2 / (1 + exp(2 u)).  Both are off
+// by a few 2^-24 of cap; in fp32 calls, whose scores may be small beside it, tanhf is not.
+constexpr float PAGED_CAP_POLY = 0.7f;
+__device__ __forceinline__ float paged_cap_poly(float cap2, float u)
 {
-    if (TY == PAGED_F32) return a.cap2 * tanhf(dot * a.inv_cap_scale);
-    return fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(dot * a.cap_in)), a.cap2);
+    const float s = u * u;
+    float p = fmaf(0.013194188f, s, -0.05019526f);
+    p = fmaf(p, s, 0.13257454f);
+    p = fmaf(p, s, -0.33326973f);
+    p = fmaf(p, s, 0.99999850f);
+    return u * cap2 * p;
 }
+__device__ __forceinline__ float paged_cap_far(float cap2, float u)
+{
+    return fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * 2.8853900817779268f)), cap2);
+}
+template <PagedType TY>
+__device__ __forceinline__ float paged_capped(float cap2, float u)
+{
+    if (TY == PAGED_F32) return cap2 * tanhf(u);
+    return fabsf(u) > PAGED_CAP_POLY ? paged_cap_far(cap2, u) : paged_cap_poly(cap2, u);
+}
+
+// q . k of a key at `far` positions from its query -> score in log2 units.  slope2: slope log2(e).
 template <PagedType TY>
 __device__ __forceinline__ float paged_score(const PagedArgs &a, float dot, float slope2, float far)
 {
-    const float x = a.cap2 == 0.0f ? dot * a.scale2 : paged_capped<TY>(a, dot);
+    const float x = a.cap2 == 0.0f ? dot * a.scale2 : paged_capped<TY>(a.cap2, dot * a.inv_cap_scale);
     return a.slopes ? fmaf(-slope2, fabsf(far), x) : x;
 }
 
@@ -99,8 +116,16 @@ __device__ __forceinline__ float paged_score(const PagedArgs &a, float dot, floa
 template <PagedType TY, int N, class V, int K, class At>
 __device__ __forceinline__ void paged_scores(const PagedArgs &a, V (&s)[K], float slope2, float far, At &&at)
 {
-    if (a.cap2 == 0.0f) unrolled<K * N>([&](auto x) { s[x / N][x % N] *= a.scale2; });
-    else unrolled<K * N>([&](auto x) { s[x / N][x % N] = paged_capped<TY>(a, s[x / N][x % N]); });
+    const float factor = a.cap2 == 0.0f ? a.scale2 : a.inv_cap_scale;
+    unrolled<K * N>([&](auto x) { s[x / N][x % N] *= factor; });
+    if (a.cap2 != 0.0f) {
+        float most = 0.0f;
+        if constexpr (TY != PAGED_F32) unrolled<K * N>([&](auto x) { most = fmaxf(most, fabsf(s[x / N][x % N])); });
+        if (TY != PAGED_F32 && !__any(most > PAGED_CAP_POLY))
+            unrolled<K * N>([&](auto x) { s[x / N][x % N] = paged_cap_poly(a.cap2, s[x / N][x % N]); });
+        else
+            unrolled<K * N>([&](auto x) { s[x / N][x % N] = paged_capped<TY>(a.cap2, s[x / N][x % N]); });
+    }
     if (a.slopes) unrolled<K * N>([&](auto x) { s[x / N][x % N] = fmaf(-slope2, fabsf(far + (float)at(x / N, x % N)), s[x / N][x % N]); });
 }
 

@@ -1,6 +1,5 @@
 // clada_paged_attn: what it accepts, and how a call is cut into workgroups.
 #include <math.h>
-#include <stdlib.h>
 
 #include "paged.h"
 
@@ -57,7 +56,6 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     a.scale2 = (float)(scores->scale * log2e);
     if (scores->cap > 0.0f) {
         a.cap2 = (float)(scores->cap * log2e);
-        a.cap_in = (float)(2.0 * log2e * scores->scale / scores->cap);
         a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
     }
     const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
@@ -69,7 +67,9 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
         const int64_t seen = (int64_t)a.window + tile / a.G;
         if (seen < keys) keys = seen;
     }
-    a.splits = clada_attn_splits(units, keys, (getenv("XW") ? atoi(getenv("XW")) : 2) * ctx->num_cu);
+    const bool eight_waves = cache->type == CLADA_PAGE_MX4 && cache->d <= 128;
+    a.splits = clada_attn_splits(units, keys, path == ATTN_ROWS && (eight_waves || cache->d >= 128) ? ctx->num_cu : 2 * ctx->num_cu);
+    a.snake = path == ATTN_TILES && units * a.splits <= 2 * ctx->num_cu;
     if (units > PAGED_MAX_ARRIVED) a.splits = 1;
     a.arrived = (int *)(ctx->ws + PAGED_ARRIVED);
     if (a.splits > 1 && (st = clada_attn_place(ctx, a)) != CLADA_OK) return st;

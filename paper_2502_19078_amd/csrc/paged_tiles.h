@@ -23,7 +23,7 @@ namespace {
 template <PagedType TY, int DP>
 struct PagedTilesShape {
     static constexpr int ES = paged_es(TY);
-    static constexpr int KT = ES == 2 && DP <= 128 ? 64 : 32;        // keys of a tile
+    static constexpr int KT = ES == 2 && DP <= 128 ? 64 : 32, KT_BITS = KT == 64 ? 6 : 5;        // keys of a tile
     static constexpr int KP = DP * ES + 16, VP = DP * ES + (ES == 2 ? 32 : 16);      // row pitches: K rows 4 banks apart, bf16 V rows 8
     static constexpr int BUF = KT * (KP + VP), LDS = 2 * BUF;
 };
@@ -49,10 +49,12 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     const PagedKV &pg = a.pg;
 
     // Units (sequence, key head) fastest: consecutive workgroups go to different XCDs, so a unit's tiles share an L2.  The last row tiles see the
-    // most keys and come first.
+    // most keys and come first; where all workgroups are resident at once, two on a compute unit, the second half comes in the other order, so that a long
+    // one shares its unit with a short one.
     const int units = a.B * a.Hkv;
     const int unit = id % units, rest = id / units;
-    const int split = rest % a.splits, tile = a.own_tiles - 1 - rest / a.splits;
+    const int split = rest % a.splits, order = rest / a.splits, half = (a.own_tiles + 1) / 2;
+    const int tile = !a.snake || order < half ? a.own_tiles - 1 - order : order - half;
     const int h = unit % a.Hkv, b = unit / a.Hkv;
     const int rows = a.T * a.G, r0 = tile * 128;
 
@@ -83,12 +85,12 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     const int low = __builtin_amdgcn_readfirstlane(min(min(s_range[0], s_range[1]), min(s_range[2], s_range[3])));
     const int high = __builtin_amdgcn_readfirstlane(max(max(s_range[4], s_range[5]), max(s_range[6], s_range[7])));
     __syncthreads();
-    const int begin = high > 0 ? low & ~15 : 0, n = high - begin;
+    const int begin = high > 0 ? low & ~(KT - 1) : 0, n = high - begin;
     int chunk = (n + a.splits - 1) / a.splits;
     chunk = (chunk + KT - 1) / KT * KT;
     const int64_t from = (int64_t)split * chunk;
     const int k0 = from < n ? begin + (int)from : high, k1 = min(k0 + min(chunk, n), high);
-    const int last16 = k1 > k0 ? (k1 - 1) & ~15 : 0;
+    const int last16 = k1 > k0 ? (k1 - 1) & ~15 : 0, last = last16 & ~(KT - 1);
 
     const unsigned int flip = !MODS && a.scale2 < 0.0f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;     // a negative scale is the queries' sign
     const float scale2 = fmaxf(fabsf(a.scale2), 0x1p-149f);  // positive, so that -inf stays what it is
@@ -106,46 +108,61 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     // A page that is not there is read as page 0 (and not used).
     const char *kp = pg.k + h * pg.sh * 16, *vp = pg.v + h * pg.sh * 16;
     const unsigned char *ksp = pg.ks + h * pg.sh, *vsp = pg.vs + h * pg.sh;
-    const int32_t *table = pg.table + b * pg.table_stride;
-    const scalar_i32 table_s = (scalar_i32)(uintptr_t)table;
+    const scalar_i32 table = (scalar_i32)(uintptr_t)(pg.table + b * pg.table_stride);
     const int in_page = (1 << pg.shift) - 1;
+    const bool one_page = pg.shift >= S::KT_BITS;            // of a tile
     const int first_key = FOUR ? tid / NG : tid / CPR, col = FOUR ? tid % NG : tid % CPR * 16;
     const bool in = FOUR ? first_key < KT : WHOLE || col < Dd * ES;
     const unsigned int lane_off = FOUR ? 0u : (unsigned int)(lane / CPR) * pg.sn * 16 + (in ? col : 0);
+    const unsigned int lane_unit = (unsigned int)(first_key & (KT - 1)) * pg.sn + (in ? col : 0);      // 4 bits
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
     unsigned int uk = 127, uv = 127;
-    int page[NB], my_page = 0;                               // of the tile that is fetched next
-    int there_next = 0, there_reg = 0, there = 0;            // a bit for every block that has a page: of that tile, of the one in registers, in LDS
+    int entry[NB];                                           // of the table, of the tile that is fetched next, as they stand there: nothing waits for them here
+    int there_reg = 0, there = 0;                            // a bit for every block that has a page: of the tile in registers, of the one in LDS
     auto look = [&](int i) {
-        there_next = 0;
+        entry[0] = table[max(min(i, one_page ? last : last16), k0) >> pg.shift];
+        if (!one_page) {
 #pragma unroll
-        for (int x = 0; x < NB; ++x) {
-            const int e = table_s[max(min(i + 16 * x, last16), k0) >> pg.shift];
-            const bool ok = (unsigned int)e < (unsigned int)pg.pages;
-            page[x] = ok ? e : 0;
-            there_next |= ok ? 1 << x : 0;
-        }
-        if constexpr (FOUR) {
-            const int e = table[max(min(i + first_key, last16), k0) >> pg.shift];
-            my_page = (unsigned int)e < (unsigned int)pg.pages ? e : 0;
+            for (int x = 1; x < NB; ++x) entry[x] = table[max(min(i + 16 * x, last16), k0) >> pg.shift];
         }
     };
     int64_t at_j[ROWS], at_u = 0;                            // where the rows of the tile that is taken lie
     auto aim = [&](int i) {
+        // (rows past the last block are read as rows of it, and those ahead of the first one as its)
+        int64_t unit[NB];
+        const bool ok = (unsigned int)entry[0] < (unsigned int)pg.pages;
+        unit[0] = paged_unit_at(pg, ok ? entry[0] : 0, max(min(i, one_page ? last : last16), k0) & in_page);
+        if (one_page) {
+            there_reg = ok ? (1 << NB) - 1 : 0;
+#pragma unroll
+            for (int x = 1; x < NB; ++x) unit[x] = unit[0] + x * 16 * (int64_t)pg.sn;
+        } else {
+            there_reg = ok;
+#pragma unroll
+            for (int x = 1; x < NB; ++x) {
+                const bool ok_x = (unsigned int)entry[x] < (unsigned int)pg.pages;
+                unit[x] = paged_unit_at(pg, ok_x ? entry[x] : 0, max(min(i + 16 * x, last16), k0) & in_page);
+                there_reg |= ok_x ? 1 << x : 0;
+            }
+        }
         if constexpr (FOUR) {
-            // (rows past the last block are read as rows of it, and those ahead of the first one as its)
-            const int p = first_key < KT ? i + first_key : i, row = max(min(p & ~15, last16), k0) + (p & 15);
-            at_u = paged_unit_at(pg, my_page, row & in_page) + (in ? col : 0);
+            if (one_page) at_u = unit[0] + (int64_t)lane_unit;
+            else {
+                const int x = (first_key & (KT - 1)) >> 4;
+                at_u = unit[0];
+#pragma unroll
+                for (int y = 1; y < NB; ++y) at_u = x == y ? unit[y] : at_u;
+                at_u += (unsigned int)(first_key & 15) * pg.sn + (in ? col : 0);
+            }
         } else
 #pragma unroll
             for (int j = 0; j < ROWS; ++j) {
                 const int first = wave * (64 / CPR) + j * RPP, x = first / 16;      // the wave's first row of the pass, and its block
-                int pj = page[0];
+                int64_t u = unit[0];
 #pragma unroll
-                for (int y = 1; y < NB; ++y) pj = x == y ? page[y] : pj;
-                at_j[j] = paged_unit_at(pg, pj, (max(min(i + 16 * x, last16), k0) & in_page) + first % 16) * 16;
+                for (int y = 1; y < NB; ++y) u = x == y ? unit[y] : u;
+                at_j[j] = (u + (first % 16) * (int64_t)pg.sn) * 16;
             }
-        there_reg = there_next;
     };
     auto take = [&](int q) {                                 // transfer q of that tile: K, V, K, ..
         if constexpr (FOUR) {
