@@ -23,6 +23,7 @@ struct PagedArgs : AttnArgs {
     int snake;                                               // order of the row tiles (paged_tiles.h)
     int tile_rows;                                           // rows of a tile: 8, 16 or 128
     float cap2, inv_cap_scale;                               // cap log2(e) (0: none), scale / cap
+    float cap_limit;                                         // products up to which a steady tile's polynomial serves (paged_tiles.h)
 };
 
 hipError_t clada_paged_launch_f32(const PagedArgs &a, AttnPath path, int num_cu, hipStream_t stream);

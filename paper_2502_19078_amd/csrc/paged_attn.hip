@@ -57,6 +57,8 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     if (scores->cap > 0.0f) {
         a.cap2 = (float)(scores->cap * log2e);
         a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
+        const float ratio = fabsf(a.inv_cap_scale);          // (the polynomial's coefficients hold its ninth power)
+        a.cap_limit = ratio >= 0x1p-12f && ratio <= 0x1p12f ? 0.7f / ratio : -1.0f;
     }
     const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
     const int tile = a.tile_rows = path == ATTN_TILES ? 128 : cache->type != CLADA_PAGE_F32 && T * a.G <= 8 ? 8 : 16;

@@ -13,7 +13,7 @@ k_paged_rows(const PagedArgs a)
     paged_rows<TY, DP, FULL, EIGHT>(a, blockIdx.x, lds);
 }
 
-template <PagedType TY, int DP, bool FULL, bool MODS>
+template <PagedType TY, int DP, bool FULL, PagedMods MODS>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 k_paged_tiles(const PagedArgs a)
 {
@@ -25,8 +25,9 @@ template <PagedType TY, int DP, bool FULL>
 void launch_paged_full(const PagedArgs &a, AttnPath path, dim3 grid, hipStream_t stream)
 {
     if (path == ATTN_TILES) {
-        if (a.cap2 != 0.0f || a.slopes) hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, true>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, false>), grid, dim3(256), 0, stream, a);
+        if (a.slopes || (TY == PAGED_F32 && a.cap2 != 0.0f)) hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, MODS_ANY>), grid, dim3(256), 0, stream, a);
+        else if (a.cap2 != 0.0f) hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, TY == PAGED_F32 ? MODS_ANY : MODS_CAP>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, MODS_NONE>), grid, dim3(256), 0, stream, a);
     } else if constexpr (TY != PAGED_F32 || DP % 64 == 0) {  // (the rows of the fp32 kernels come in 64 values)
         if (TY != PAGED_F32 && a.tile_rows == 8) hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, TY != PAGED_F32>), grid, dim3(64 * PagedRowsShape<TY, DP, FULL>::WAVES), 0, stream, a);
         else hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, false>), grid, dim3(64 * PagedRowsShape<TY, DP, FULL>::WAVES), 0, stream, a);

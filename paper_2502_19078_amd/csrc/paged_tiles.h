@@ -24,12 +24,14 @@ template <PagedType TY, int DP>
 struct PagedTilesShape {
     static constexpr int ES = paged_es(TY);
     static constexpr int KT = ES == 2 && DP <= 128 ? 64 : 32, KT_BITS = KT == 64 ? 6 : 5;        // keys of a tile
-    static constexpr int KP = DP * ES + 16, VP = DP * ES + (ES == 2 ? 32 : 16);      // row pitches: K rows 4 banks apart, bf16 V rows 8
+    static constexpr int KP = DP * ES + 16, VP = DP * ES + (ES == 4 ? 16 : DP % 64 ? 0 : 64);      // row pitches: K rows 4 banks apart, bf16 V rows 16 or 48
     static constexpr int BUF = KT * (KP + VP), LDS = 2 * BUF;
 };
 
-// MODS: the scores have a cap or a slope.
-template <PagedType TY, int DP, bool FULL, bool MODS>
+// What the scores have beside a scale: nothing, a cap alone (not in fp32), anything.
+enum PagedMods { MODS_NONE, MODS_CAP, MODS_ANY };
+
+template <PagedType TY, int DP, bool FULL, PagedMods MODS>
 __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, char *lds)
 {
     using S = PagedTilesShape<TY, DP>;
@@ -64,7 +66,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     int len, qlen;
     sequence_lens(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.T, len, qlen);
     const RowSpan span = paged_span(a, b, token, len, qlen);
-    const float slope2 = MODS ? paged_slope2(a, h * a.G + rc - token * a.G) : 0.0f;
+    const float slope2 = MODS == MODS_ANY ? paged_slope2(a, h * a.G + rc - token * a.G) : 0.0f;
     int any0 = !idle && span.begin < span.end ? span.begin : INT32_MAX, any1 = idle ? 0 : span.end, all0 = span.begin, all1 = span.end;
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) {
@@ -92,7 +94,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     const int k0 = from < n ? begin + (int)from : high, k1 = min(k0 + min(chunk, n), high);
     const int last16 = k1 > k0 ? (k1 - 1) & ~15 : 0, last = last16 & ~(KT - 1);
 
-    const unsigned int flip = !MODS && a.scale2 < 0.0f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;     // a negative scale is the queries' sign
+    const unsigned int flip = MODS == MODS_NONE && a.scale2 < 0.0f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;     // a negative scale is the queries' sign
     const float scale2 = fmaxf(fabsf(a.scale2), 0x1p-149f);  // positive, so that -inf stays what it is
     u32x4 qf[KD];
 #pragma unroll
@@ -184,15 +186,19 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
 #pragma unroll
         for (int q = 0; q < 2 * ROWS; ++q) take(q);
     };
-    // (threads without a chunk write into the row's padding; 4 bits: threads without a row write nothing)
-    const unsigned int put_k = first_key * KP + (FOUR ? col * 64 : min(col, DP * ES)), put_v = KT * KP + first_key * VP + (FOUR ? col * 64 : min(col, DP * ES));
+    // (threads without a chunk write into the padding of a row of K and no V; 4 bits: threads without a row write nothing)
+    // The 16-byte chunks of each 64 bytes of a row of bf16 V change places by the row, so that neither the reads nor the writes of four rows meet in a
+    // bank (with rows 8 banks apart and no turn the waits for LDS took a quarter of its time).
+    const unsigned int put_at = FOUR ? col * 64 : min(col, DP * ES), turn = ES == 2 ? (first_key & 3) * 16 : 0;
+    const unsigned int put_k = first_key * KP + put_at, put_v = KT * KP + first_key * VP + (FOUR ? put_at : put_at ^ turn);
     auto put_one = [&](int buf, int q) {                     // write q into LDS
         if constexpr (FOUR) {
             if (KT * NG < 256 && !in) return;
             const int c = q & 3;
-            char *to = lds + ((q & 4 ? put_v : put_k) + buf * BUF) + c * 16;
+            char *to = lds + ((q & 4 ? put_v : put_k) + buf * BUF) + (q & 4 ? c * 16 ^ turn : c * 16);
             *reinterpret_cast<u32x4 *>(to) = q & 4 ? paged_bf16x8(sv[0][c], paged_scale(uv)) : paged_bf16x8(sk[0][c], paged_scale(uk));
         } else {
+            if ((q & 1) && CPR * 16 > DP * ES && col >= DP * ES) return;
             const int j = q / 2;
             u32x4 x = q & 1 ? sv[j] : sk[j];
             if (!WHOLE && !in) x = u32x4{0, 0, 0, 0};
@@ -223,6 +229,17 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+    // MODS_CAP: a steady tile takes cap2 tanh(x kappa) as x times a polynomial of x^2, x the product.
+    float cap_k[5] = {};
+    if constexpr (MODS == MODS_CAP) {
+        constexpr float coeff[5] = {0.99999850f, -0.33326973f, 0.13257454f, -0.05019526f, 0.013194188f};
+        float f = a.cap2 * a.inv_cap_scale;
+#pragma unroll
+        for (int c = 0; c < 5; ++c) {
+            cap_k[c] = f * coeff[c];
+            f *= a.inv_cap_scale * a.inv_cap_scale;
+        }
+    }
     // One tile for this wave's rows.  EDGE: some of them do not see all of it, or a maximum has to be set or moved.  Otherwise the next tile goes
     // into LDS, and the one behind it is taken, transfer by transfer between the products; false, and nothing has been done, where a maximum has to be moved.
     auto multiply = [&](auto edge, int i, int buf) -> bool {
@@ -264,7 +281,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
             __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MODS) paged_scores<TY, 16>(a, s, slope2, (float)(i + 4 * hh - span.pos), [](int k, int e) { return k * 32 + 8 * (e >> 2) + (e & 3); });
+        if constexpr (MODS == MODS_ANY || (MODS == MODS_CAP && EDGE)) paged_scores<TY, 16>(a, s, slope2, (float)(i + 4 * hh - span.pos), [](int k, int e) { return k * 32 + 8 * (e >> 2) + (e & 3); });
         if constexpr (EDGE) {
             const int lo = span.begin - i - 4 * hh;
             const unsigned int width = (unsigned int)max(min(span.end, k1) - span.begin, 0);
@@ -276,12 +293,13 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
                     s[k][e] = seen ? s[k][e] : NEG_INF;
                 }
         }
-        float top = NEG_INF;
+        constexpr bool BOUND = MODS == MODS_CAP && !EDGE;    // the largest magnitude of a product in place of the largest score
+        float top = BOUND ? 0.0f : NEG_INF;
 #pragma unroll
         for (int k = 0; k < KB; ++k)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
-        if (!MODS) top *= scale2;
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, BOUND ? fabsf(s[k][e]) : s[k][e]);
+        if (MODS == MODS_NONE) top *= scale2;
         if constexpr (EDGE) {
             if (__any(top > m + 8.0f)) {                     // (weights above 1 lose nothing)
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -293,13 +311,24 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
                 for (int d = 0; d < DB; ++d) o[d] *= f;
             }
         } else {
-            if (__any(top > m + 32.0f)) return false;
+            if (BOUND ? __any(top > a.cap_limit || top * fabsf(cap_k[0]) > m + 32.0f) : __any(top > m + 32.0f)) return false;
             there = there_reg;
             aim(i - 2 * KT);
             look(i - 3 * KT);
         }
         const float base = m == NEG_INF ? 0.0f : m;
-        auto weight_of = [&](float x) { return MODS ? __builtin_amdgcn_exp2f(x - base) : __builtin_amdgcn_exp2f(fmaf(x, scale2, -base)); };
+        auto weight_of = [&](float x) {
+            if constexpr (MODS == MODS_NONE) return __builtin_amdgcn_exp2f(fmaf(x, scale2, -base));
+            if constexpr (BOUND) {
+                const float x2 = x * x;
+                float y = fmaf(cap_k[4], x2, cap_k[3]);
+                y = fmaf(y, x2, cap_k[2]);
+                y = fmaf(y, x2, cap_k[1]);
+                y = fmaf(y, x2, cap_k[0]);
+                return __builtin_amdgcn_exp2f(fmaf(x, y, -base));
+            }
+            return __builtin_amdgcn_exp2f(x - base);
+        };
         if constexpr (ES == 2) {
             // Sixteen keys are a step of the second product.  Between the products of one step stand the exponentials of the next one and the
             // reads of V four products ahead.
@@ -312,7 +341,8 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
                 s[k][8 * c + e] = p;
                 if (e & 1) pk[st & 1][e >> 1] = pack_bf16(s[k][8 * c + e - 1], p);
             };
-            const char *src = vb + (4 * hh + (t16 >> 2)) * VP + (g & 1) * 32 + (t16 & 3) * 8;
+            // (row 4 hh + t16 / 4 of each 8, whose chunks are turned by t16 / 4)
+            const char *src = vb + (4 * hh + (t16 >> 2)) * VP + ((((g & 1) * 2 + (t16 >> 1 & 1)) ^ (t16 >> 2)) * 16) + (t16 & 1) * 8;
             auto read_v = [&](int x) {
                 const char *at = src + x / DB * 16 * VP + x % DB * 64;
                 const uint2 u0 = read_tr16(at), u1 = read_tr16(at + 8 * VP);
