@@ -45,7 +45,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     constexpr int PUTS = FOUR ? 8 : 2 * ROWS;                // 16-byte writes into LDS a thread and tile
     static_assert(FOUR ? KT * NG <= 256 : KT * CPR % 256 == 0 && 256 % CPR == 0, "whole passes");
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
     const int n32 = lane & 31, hh = lane >> 5, t16 = lane & 15, g = lane >> 4;
     const int Dd = FULL ? DP : a.D;
     const PagedKV &pg = a.pg;
@@ -105,6 +105,9 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
 #pragma unroll
         for (int e = 0; e < 4; ++e) qf[c][e] = in ? qf[c][e] ^ flip : 0u;
     }
+    // (here, once: a wait for them inside the loop would be one for the tiles on their way too)
+#pragma unroll
+    for (int c = 0; c < KD; ++c) asm volatile("" : "+v"(qf[c]));
 
     // Staging.  16 and 32 bits: a wave's rows of a pass lie in one 16-key block, whose page is a scalar; 4 bits: a thread has one row of K and of V.
     // A page that is not there is read as page 0 (and not used).
@@ -117,6 +120,9 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     const bool in = FOUR ? first_key < KT : WHOLE || col < Dd * ES;
     const unsigned int lane_off = FOUR ? 0u : (unsigned int)(lane / CPR) * pg.sn * 16 + (in ? col : 0);
     const unsigned int lane_unit = (unsigned int)(first_key & (KT - 1)) * pg.sn + (in ? col : 0);      // 4 bits
+    int64_t step[ROWS];                                      // of a pass, in a tile of one page
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) step[j] = (int64_t)(wave * (64 / CPR) + j * RPP) * pg.sn * 16;
     u32x4 sk[ROWS], sv[ROWS];                                // the tile on its way into LDS
     unsigned int uk = 127, uv = 127;
     int entry[NB];                                           // of the table, of the tile that is fetched next, as they stand there: nothing waits for them here
@@ -131,31 +137,31 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     int64_t at_j[ROWS], at_u = 0;                            // where the rows of the tile that is taken lie
     auto aim = [&](int i) {
         // (rows past the last block are read as rows of it, and those ahead of the first one as its)
-        int64_t unit[NB];
-        const bool ok = (unsigned int)entry[0] < (unsigned int)pg.pages;
-        unit[0] = paged_unit_at(pg, ok ? entry[0] : 0, max(min(i, one_page ? last : last16), k0) & in_page);
+        constexpr int ALL = (1 << NB) - 1;
         if (one_page) {
-            there_reg = ok ? (1 << NB) - 1 : 0;
+            const bool ok = (unsigned int)entry[0] < (unsigned int)pg.pages;
+            there_reg = ok ? ALL : 0;
+            const int64_t unit = paged_unit_at(pg, ok ? entry[0] : 0, max(min(i, last), k0) & in_page);
+            if constexpr (FOUR) at_u = unit + (int64_t)lane_unit;
+            else
 #pragma unroll
-            for (int x = 1; x < NB; ++x) unit[x] = unit[0] + x * 16 * (int64_t)pg.sn;
-        } else {
-            there_reg = ok;
+                for (int j = 0; j < ROWS; ++j) at_j[j] = (unit << 4) + step[j];
+            return;
+        }
+        int64_t unit[NB];
+        there_reg = 0;
 #pragma unroll
-            for (int x = 1; x < NB; ++x) {
-                const bool ok_x = (unsigned int)entry[x] < (unsigned int)pg.pages;
-                unit[x] = paged_unit_at(pg, ok_x ? entry[x] : 0, max(min(i + 16 * x, last16), k0) & in_page);
-                there_reg |= ok_x ? 1 << x : 0;
-            }
+        for (int x = 0; x < NB; ++x) {
+            const bool ok = (unsigned int)entry[x] < (unsigned int)pg.pages;
+            unit[x] = paged_unit_at(pg, ok ? entry[x] : 0, max(min(i + 16 * x, last16), k0) & in_page);
+            there_reg |= ok ? 1 << x : 0;
         }
         if constexpr (FOUR) {
-            if (one_page) at_u = unit[0] + (int64_t)lane_unit;
-            else {
-                const int x = (first_key & (KT - 1)) >> 4;
-                at_u = unit[0];
+            const int x = (first_key & (KT - 1)) >> 4;
+            at_u = unit[0];
 #pragma unroll
-                for (int y = 1; y < NB; ++y) at_u = x == y ? unit[y] : at_u;
-                at_u += (unsigned int)(first_key & 15) * pg.sn + (in ? col : 0);
-            }
+            for (int y = 1; y < NB; ++y) at_u = x == y ? unit[y] : at_u;
+            at_u += (unsigned int)(first_key & 15) * pg.sn + (in ? col : 0);
         } else
 #pragma unroll
             for (int j = 0; j < ROWS; ++j) {
@@ -257,28 +263,25 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
         };
         f32x16 s[KB];
         const f32x16 zero = {};
+        constexpr int QKS = KD * KB, KA = QKS < 6 ? QKS : 6; // fragments of K ahead of the products
+        u32x4 kf[KA];
+        const char *k_lane = kb + n32 * KP + 16 * hh;
+        auto read_k = [&](int x) { kf[x % KA] = *reinterpret_cast<const u32x4 *>(k_lane + x % KB * (32 * KP) + x / KB * 32); };
 #pragma unroll
-        for (int c = 0; c < KD; ++c)
+        for (int x = 0; x < KA; ++x) read_k(x);
 #pragma unroll
-            for (int k = 0; k < KB; ++k) {
-                const u32x4 kf = *reinterpret_cast<const u32x4 *>(kb + (k * 32 + n32) * KP + 32 * c + 16 * hh);
-                if constexpr (ES == 2)
-                    s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
-                else
+        for (int x = 0; x < QKS; ++x) {
+            const int c = x / KB, k = x % KB;
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (ES == 2)
+                s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x % KA]), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
+            else
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned int ka = kf[e], qb = qf[c][e];
-                        s[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka), __uint_as_float(qb), c || e ? s[k] : zero, 0, 0, 0);
-                    }
-            }
-        if constexpr (ES == 2 && KD * KB >= 8) {             // six fragments ahead of the products
-            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-            for (int x = 0; x < KD * KB - 6; ++x) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned int ka = kf[x % KA][e], qb = qf[c][e];
+                    s[k] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka), __uint_as_float(qb), c || e ? s[k] : zero, 0, 0, 0);
+                }
+            if (x + KA < QKS) read_k(x + KA);
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (MODS == MODS_ANY || (MODS == MODS_CAP && EDGE)) paged_scores<TY, 16>(a, s, slope2, (float)(i + 4 * hh - span.pos), [](int k, int e) { return k * 32 + 8 * (e >> 2) + (e & 3); });
@@ -396,6 +399,8 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
         look(i - 2 * KT);
     }
     tile_barrier();
+    // Where a tile is seen by all rows of the wave and the next one has no row that nobody sees.
+    const int steady0 = max(all0, max(low, k0) + KT), steady1 = min(all1, k1) - KT;
     // The waves of a workgroup may be in different loops; every tile is one barrier in both.
     while (i >= k0) {
         if (i < wave1 && i + KT > wave0) multiply(std::true_type{}, i, buf);
@@ -408,8 +413,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
             tile_barrier();
             buf ^= 1;
             i -= KT;
-            // all of the tile seen by all rows of the wave, and the next one free of rows that nobody sees
-            if (i < max(all0, k0) || i + KT > min(all1, k1) || there != (1 << NB) - 1 || i - KT < k0 || !clean(i - KT)) break;
+            if (i < steady0 || i > steady1 || (there & there_reg) != (1 << NB) - 1) break;
             if (!multiply(std::false_type{}, i, buf)) break;
         }
     }
