@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -561,6 +562,15 @@ def attn_workspace_bytes(B: int, T: int, Hq: int, d: int) -> int:
     return int(load_library().clada_attn_workspace_bytes(B, T, Hq, d))
 
 
+# The small structs of these calls as bytes, laid out as the classes above: packing costs a third of filling a ctypes structure, and single tokens
+# wait for it.
+_PACK_HEADS = struct.Struct("@Pqqq").pack                                    # _CHeads
+_PACK_ROPE = struct.Struct("@Piif4x").pack                                   # _CRope
+_PACK_NORM = struct.Struct("@PPff").pack                                     # _CHeadNorm
+_PACK_PAGED = struct.Struct("@PPPPqqqPqiiiiiii4x").pack                      # _CPagedCache
+_PACK_SCORES = struct.Struct("@ffPPPi4x").pack                               # _CAttnScores
+
+
 class KVCache:
     """Keys and values [batch][heads][capacity][d] on the GPU: two tensors (views with any strides, d contiguous) of one shape and one
     set of strides.  ring = 0: row n holds position n.  ring > 0: positions from n_sink on share `ring` rows behind the first n_sink."""
@@ -583,7 +593,7 @@ def _heads(x: torch.Tensor, shape, cache: KVCache, what: str):
     sb, st, sh, sd = x.stride()
     assert x.get_device() == cache.device_index and x.dtype is cache.dtype and sd == 1 and shape[3] == cache.d, \
         f"{what}: type, device, head size or strides do not fit the cache"
-    return C.byref(_CHeads(x.data_ptr(), sb if shape[0] > 1 else 0, st if shape[1] > 1 else 0, sh if shape[2] > 1 else 0))
+    return _PACK_HEADS(x.data_ptr(), sb if shape[0] > 1 else 0, st if shape[1] > 1 else 0, sh if shape[2] > 1 else 0)
 
 
 def _ints(x: torch.Tensor, n: int, cache: KVCache, what: str):
@@ -632,8 +642,8 @@ def _rope_args(plan: RopePlan, q, k, v, cache, q_norm, k_norm, eps, norm_offset,
     if norm or (norm is None and (q_norm is not None or k_norm is not None)):
         for w in (q_norm, k_norm):
             assert w is None or (w.get_device() == cache.device_index and w.dtype is cache.dtype and w.is_contiguous() and w.numel() == cache.d)
-        c_norm = C.byref(_CHeadNorm(_ptr(q_norm), _ptr(k_norm), eps, norm_offset))
-    return (x, out, B, T, Hq, C.byref(_CRope(turns.data_ptr(), 2 * turns.numel(), plan.layout, plan.magnitude)), c_norm, cq, ck, cv, co)
+        c_norm = _PACK_NORM(0 if q_norm is None else q_norm.data_ptr(), 0 if k_norm is None else k_norm.data_ptr(), eps, norm_offset)
+    return x, out, B, T, Hq, _PACK_ROPE(turns.data_ptr(), 2 * turns.numel(), plan.layout, plan.magnitude), c_norm, cq, ck, cv, co
 
 
 def qk_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
@@ -686,31 +696,32 @@ class PagedCache:
     """Pages [pages][heads][page_size][d] of a pool on the GPU (k and v: views with one set of strides, d contiguous), fp32 or bf16, or in 4 bits: k and v
     uint8 [..][d/2] with scales uint8 [..][d/32], whose strides are those of the values over 32.  table [batch][max_pages] int32 (rows contiguous) names
     the pages of every sequence; an entry outside the pool names none."""
-    __slots__ = ("k", "v", "k_scales", "v_scales", "table", "heads", "d", "dtype", "device_index", "_c", "_ref")
+    __slots__ = ("k", "v", "k_scales", "v_scales", "table", "heads", "d", "dtype", "device_index", "_c")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None):
-        shape, stride, four = k.shape, k.stride(), k.dtype is torch.uint8
-        assert k.is_cuda and len(shape) == 4 and v.shape == shape and v.dtype is k.dtype and v.get_device() == k.get_device()
+        shape, stride, dtype, device = k.shape, k.stride(), k.dtype, k.get_device()
+        assert device >= 0 and len(shape) == 4 and v.shape == shape and v.dtype is dtype and v.get_device() == device
         assert stride[3] == 1 and v.stride() == stride, "k and v need one set of strides, the values of a row contiguous"
-        assert table.dtype is torch.int32 and table.dim() == 2 and table.stride(1) == 1 and table.get_device() == k.get_device()
+        (B, per), (table_stride, one) = table.shape, table.stride()
+        assert table.dtype is torch.int32 and one == 1 and table.get_device() == device
         P, H, S, D = shape
-        sizes = [stride[0] if P > 1 else 0, stride[1] if H > 1 else 0, stride[2]]
-        if four:
+        sp, sh, sn = stride[0] if P > 1 else 0, stride[1] if H > 1 else 0, stride[2]
+        ks = vs = 0
+        if dtype is torch.uint8:
             assert D % 16 == 0, "rows of 4 bits hold a multiple of 32 values"
             for x in (k_scales, v_scales):
-                assert x is not None and x.dtype is torch.uint8 and x.shape == (P, H, S, D // 16) and x.get_device() == k.get_device()
+                assert x is not None and x.dtype is torch.uint8 and x.shape == (P, H, S, D // 16) and x.get_device() == device
                 assert all(n == 1 or 16 * a == b for n, a, b in zip((P, H, S), x.stride(), stride)) and x.stride(3) == 1, \
                     "the scales need the strides of the values over 32"
-            sizes, D = [2 * n for n in sizes], 2 * D
+            sp, sh, sn, D, kind, ks, vs = 2 * sp, 2 * sh, 2 * sn, 2 * D, PAGE_MX4, k_scales.data_ptr(), v_scales.data_ptr()
+            dtype = torch.bfloat16
         else:
             assert k_scales is None and v_scales is None
+            kind = PAGE_F32 if _dtype_code(k) == F32 else PAGE_BF16
         self.k, self.v, self.k_scales, self.v_scales, self.table = k, v, k_scales, v_scales, table
-        self.heads, self.d, self.device_index = H, D, k.get_device()
-        self.dtype = torch.bfloat16 if four else k.dtype          # of queries, new rows and outputs
-        B, per = table.shape
-        self._c = _CPagedCache(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), *sizes, table.data_ptr(), table.stride(0) if B > 1 else per,
-                               P, H, S, D, B, per, PAGE_MX4 if four else PAGE_F32 if _dtype_code(k) == F32 else PAGE_BF16)
-        self._ref = C.byref(self._c)
+        self.heads, self.d, self.device_index = H, D, device
+        self.dtype = dtype                                        # of queries, new rows and outputs
+        self._c = _PACK_PAGED(k.data_ptr(), v.data_ptr(), ks, vs, sp, sh, sn, table.data_ptr(), table_stride if B > 1 else per, P, H, S, D, B, per, kind)
 
 
 def paged_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
@@ -718,7 +729,7 @@ def paged_rope(ctx: Context, plan: RopePlan, q: torch.Tensor | None, k: torch.Te
                norm: bool | None = None, out: torch.Tensor | None = None):
     """qk_rope into pages: token (b, t) is stored at positions[b][t] of sequence b (negative: padding)."""
     x, out, B, T, Hq, plan_c, norm_c, cq, ck, cv, co = _rope_args(plan, q, k, v, cache, q_norm, k_norm, eps, norm_offset, norm, out)
-    ctx.check(ctx._lib.clada_paged_rope(ctx._h, plan_c, norm_c, B, T, Hq, cq, ck, cv, _ints(positions, B * T, cache, "positions"), co, cache._ref, _stream(x)))
+    ctx.check(ctx._lib.clada_paged_rope(ctx._h, plan_c, norm_c, B, T, Hq, cq, ck, cv, _ints(positions, B * T, cache, "positions"), co, cache._c, _stream(x)))
     return out if q is not None else None
 
 
@@ -731,7 +742,7 @@ def paged_read(ctx: Context, cache: PagedCache, positions: torch.Tensor, k_out: 
     for x in (k_out, v_out):
         assert x is None or x.shape == shape
     B, T = positions.shape
-    ctx.check(ctx._lib.clada_paged_read(ctx._h, cache._ref, _ints(positions, B * T, cache, "positions"), B, T,
+    ctx.check(ctx._lib.clada_paged_read(ctx._h, cache._c, _ints(positions, B * T, cache, "positions"), B, T,
                                         None if k_out is None else _heads(k_out, shape, cache, "k_out"),
                                         None if v_out is None else _heads(v_out, shape, cache, "v_out"), _stream(positions)))
     return k_out, v_out
@@ -751,11 +762,12 @@ def paged_attn(ctx: Context, q: torch.Tensor, cache: PagedCache, lens: torch.Ten
         assert out.shape == shape
     assert slopes is None or (slopes.dtype is torch.float32 and slopes.numel() == Hq and slopes.is_contiguous() and slopes.get_device() == cache.device_index)
     lse = torch.empty((B, T, Hq), dtype=torch.float32, device=q.device) if want_lse else None
-    c = _CAttnScores(D ** -0.5 if scale is None else scale, cap, _ptr(slopes), None if prefix_lens is None else _ints(prefix_lens, B, cache, "prefix_lens"),
-                     None if first is None else _ints(first, B * T, cache, "first"), window)
-    ctx.check(ctx._lib.clada_paged_attn(ctx._h, _heads(q, shape, cache, "q"), cache._ref, _ints(lens, B, cache, "lens"),
-                                        None if q_lens is None else _ints(q_lens, B, cache, "q_lens"), B, T, Hq, max_len, C.byref(c),
-                                        _heads(out, shape, cache, "out"), _ptr(lse), _stream(q)))
+    c = _PACK_SCORES(D ** -0.5 if scale is None else scale, cap, 0 if slopes is None else slopes.data_ptr(),
+                     0 if prefix_lens is None else _ints(prefix_lens, B, cache, "prefix_lens"), 0 if first is None else _ints(first, B * T, cache, "first"),
+                     window)
+    ctx.check(ctx._lib.clada_paged_attn(ctx._h, _heads(q, shape, cache, "q"), cache._c, _ints(lens, B, cache, "lens"),
+                                        None if q_lens is None else _ints(q_lens, B, cache, "q_lens"), B, T, Hq, max_len, c,
+                                        _heads(out, shape, cache, "out"), None if lse is None else lse.data_ptr(), _stream(q)))
     return (out, lse) if want_lse else out
 
 

@@ -272,6 +272,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
 #pragma unroll
         for (int x = 0; x < QKS; ++x) {
             const int c = x / KB, k = x % KB;
+            if (TY == PAGED_F32 && !FULL && 32 * c >= Dd * ES) continue;      // (fp32: nothing but the products' own time counts)
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (ES == 2)
                 s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x % KA]), __builtin_bit_cast(bf16x8, qf[c]), c ? s[k] : zero, 0, 0, 0);
