@@ -5,12 +5,12 @@
 
 namespace {
 
-template <PagedType TY, int DP, bool FULL, bool EIGHT>
+template <PagedType TY, int DP, bool FULL, bool EIGHT, bool ALONE>
 __global__ void __launch_bounds__((64 * PagedRowsShape<TY, DP, FULL>::WAVES), TY == PAGED_4BIT && DP <= 128 ? 4 : TY != PAGED_F32 || DP <= 128 ? 2 : 1)
 k_paged_rows(const PagedArgs a)
 {
     __shared__ __align__(16) char lds[PagedRowsShape<TY, DP, FULL>::LDS];
-    paged_rows<TY, DP, FULL, EIGHT>(a, blockIdx.x, lds);
+    paged_rows<TY, DP, FULL, EIGHT, ALONE>(a, blockIdx.x, lds);
 }
 
 template <PagedType TY, int DP, bool FULL, PagedMods MODS>
@@ -29,8 +29,10 @@ void launch_paged_full(const PagedArgs &a, AttnPath path, dim3 grid, hipStream_t
         else if (a.cap2 != 0.0f) hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, TY == PAGED_F32 ? MODS_ANY : MODS_CAP>), grid, dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((k_paged_tiles<TY, DP, FULL, MODS_NONE>), grid, dim3(256), 0, stream, a);
     } else if constexpr (TY != PAGED_F32 || DP % 64 == 0) {  // (the rows of the fp32 kernels come in 64 values)
-        if (TY != PAGED_F32 && a.tile_rows == 8) hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, TY != PAGED_F32>), grid, dim3(64 * PagedRowsShape<TY, DP, FULL>::WAVES), 0, stream, a);
-        else hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, false>), grid, dim3(64 * PagedRowsShape<TY, DP, FULL>::WAVES), 0, stream, a);
+        const dim3 block(64 * PagedRowsShape<TY, DP, FULL>::WAVES);
+        if (TY != PAGED_F32 && a.tile_rows == 8) hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, TY != PAGED_F32, true>), grid, block, 0, stream, a);
+        else if (a.own_tiles == 1) hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, false, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_paged_rows<TY, DP, FULL, false, false>), grid, block, 0, stream, a);
     }
 }
 

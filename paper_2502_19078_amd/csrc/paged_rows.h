@@ -119,13 +119,25 @@ __device__ __forceinline__ void paged_join(const PagedArgs &a, const int unit, c
     }
 }
 
+// Rows that no other workgroup reads pass by the caches: 32 x 8000 tokens of 8 heads in bf16 186 us, 212 by ordinary loads; one sequence of 131071 in 4
+// bits 30.8, 33.3.  Rows that several tiles read do not (64 heads on one key head, 8 x 32000 in bf16: 64 us so, 52 by ordinary loads), nor rows
+// shorter than half a cache line, whose line is another head's too (24 x 9000 in 4 bits, 64 values a head: 27.8, 25.0).
+template <bool ONCE, class T>
+__device__ __forceinline__ T read_row(const T *p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
 // EIGHT: tiles of 8 rows.  The other 8 columns of the products hold the same rows, with the lower halves of the weights in the second one.
-template <PagedType TY, int DP, bool FULL, bool EIGHT>
+// ALONE: one tile holds all rows of a key head.
+template <PagedType TY, int DP, bool FULL, bool EIGHT, bool ALONE>
 __device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, char *lds)
 {
     using S = PagedRowsShape<TY, DP, FULL>;
     constexpr int ES = paged_es(TY);
     constexpr bool FOUR = TY == PAGED_4BIT;
+    constexpr bool ONCE = ALONE && (!FOUR || DP >= 128);
     constexpr int KB = S::KB, KS = S::KS, PITCH = S::PITCH, WAVES = S::WAVES, TILE = EIGHT ? 8 : 16;
     constexpr int NW = DP / 32;                              // 4 bits: words of a quarter of a row; also its chunks of 8 values
     constexpr int CH = FOUR ? NW : DP * ES / 64;             // operand chunks of a row: 16 bytes of every lane group each
@@ -237,7 +249,7 @@ __device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, 
         for (int kb = 0; kb < KB; ++kb) {
             const char *p = kp + unit[kb] * 16;
             if constexpr (FOUR) {
-                kc[kb] = *reinterpret_cast<const typename Words<NW>::type *>(p + (lane_row * 16 + (unsigned int)(g * (DP / 8))));
+                kc[kb] = read_row<ONCE>(reinterpret_cast<const typename Words<NW>::type *>(p + (lane_row * 16 + (unsigned int)(g * (DP / 8)))));
 #pragma unroll
                 for (int j = 0; j < NU; ++j) ku[kb][j] = (ksp + unit[kb])[lane_row + (unsigned int)min(scale0 + j, NW - 1)];
             } else
@@ -245,7 +257,7 @@ __device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, 
                 for (int c = 0; c < CH; ++c) {
                     const int off = 64 * c + 16 * g;
                     const bool in = FULL || off < Dd * ES;
-                    kf[kb][c] = *reinterpret_cast<const u32x4 *>(p + (lane_row * 16 + (unsigned int)(in ? off : 0)));
+                    kf[kb][c] = read_row<ONCE>(reinterpret_cast<const u32x4 *>(p + (lane_row * 16 + (unsigned int)(in ? off : 0))));
                     if (!in) kf[kb][c] = u32x4{0, 0, 0, 0};
                 }
         }
@@ -254,7 +266,7 @@ __device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, 
         if constexpr (FOUR) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                vc[kb] = *reinterpret_cast<const typename Words<NW>::type *>(vp + unit[kb] * 16 + (lane_row * 16 + (unsigned int)(g * (DP / 8))));
+                vc[kb] = read_row<ONCE>(reinterpret_cast<const typename Words<NW>::type *>(vp + unit[kb] * 16 + (lane_row * 16 + (unsigned int)(g * (DP / 8)))));
 #pragma unroll
                 for (int j = 0; j < NU; ++j) vu[kb][j] = (vsp + unit[kb])[lane_row + (unsigned int)min(scale0 + j, NW - 1)];
             }
@@ -265,7 +277,7 @@ __device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, 
                 const int kb = ES == 2 ? j / PER : 0, x = ES == 2 ? lane + 64 * (j % PER) : 0;
                 const int key = ES == 2 ? x / CPR : 4 * g + j % 4, col = ES == 2 ? x % CPR : 16 * (j / 4) + n16;
                 const bool in = FULL || col * 16 < Dd * ES;
-                vf[j] = *reinterpret_cast<const u32x4 *>(vp + unit[kb] * 16 + ((unsigned int)key * pg.sn * 16 + (unsigned int)(in ? col * 16 : 0)));
+                vf[j] = read_row<ONCE>(reinterpret_cast<const u32x4 *>(vp + unit[kb] * 16 + ((unsigned int)key * pg.sn * 16 + (unsigned int)(in ? col * 16 : 0))));
                 if (!in) vf[j] = u32x4{0, 0, 0, 0};
             }
     };
