@@ -524,8 +524,8 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
  * Position p of sequence b lies in row p % page_size of page table[b][p / page_size].  An entry outside [0, pages) names no page: its
  * positions are not stored, read as zeros, and are seen by no query; so are positions from max_pages * page_size on.  Sequences may share
  * pages that no call stores into.  k and v are [pages][heads][page_size][d] of one set of strides (elements; multiples of 16 bytes, 32
- * values for CLADA_PAGE_MX4), the d values of a row contiguous; page_size is a power of two from 16 to 4096; table (device) has rows of
- * table_stride entries.
+ * values for CLADA_PAGE_MX4; stride_n at most 2^26, stride_p at most 2^33), the d values of a row contiguous; page_size is a power of two
+ * from 16 to 4096; table (device) has rows of table_stride entries.
  *
  * CLADA_PAGE_MX4 holds a value in 4 bits (d a multiple of 32): 32 neighbours of a row share a power of two, 2^(byte - 127) with one byte in
  * k_scales / v_scales (byte 255: all 32 are NaN), and a value is 0, 0.5, 1, 1.5, 2, 3, 4 or 6 of it, codes 0 to 7, with 8 added for a

@@ -56,8 +56,8 @@ struct ReadArgs {
 };
 
 // A thread for 16 bytes that are written, of READ_TOKENS tokens one behind the other, whose pages and rows are on their way together; eight values of
-// 4 bits are one word.  Bound by the bytes of both sides (HBM): 4 x 4001 rows of 8 heads of 128 values out of 4 bits 14 us, 4.6 TB/s (22 with
-// a token a thread and its place by division of 64 bits).
+// 4 bits are one word.  Bound by the bytes of both sides (HBM): 4 x 4001 rows of 8 heads of 128 values out of 4 bits 15.4 us, 4.2 TB/s (20.7
+// with a token a thread and its place by division of 64 bits; 21.8 with loads that pass by the caches).
 constexpr int READ_TOKENS = 4;
 template <PagedType TY>
 __global__ void __launch_bounds__(256)

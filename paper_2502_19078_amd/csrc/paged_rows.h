@@ -3,12 +3,14 @@
 // For a row r and the keys p that it sees:  o_r = sum_p exp(s_rp - lse_r) v_p,  lse_r = log sum_p exp(s_rp), s as paged_score says.  One pass over
 // the keys with a running maximum and sum per row, in base 2.
 //
-// Bound by the pages' bytes (HBM): a key head's rows are read once for all query heads of its group.  A workgroup takes a tile of 16 rows and
-// one split of their keys; its four waves (eight where rows are short) take steps of 16 or 32 keys in turn, each with a running softmax of its own, so nothing waits
-// inside the loop; the waves' results are joined through LDS, those of the splits by k_attn_join.
+// Bound by the pages' bytes (HBM): a key head's rows are read once for all query heads of its group.  A workgroup takes a tile of 8 or 16 rows and
+// one split of their keys; its four waves (eight for rows of 4 bits) take steps of 16 or 32 keys in turn, each with a running softmax of its
+// own, so nothing waits inside the loop; the waves' results are joined through LDS, those of the splits by the last workgroup to arrive.
+// Rows of 4 bits are bound by what is done to a key beside its bytes: about 160 vector instructions for 32 keys of 64 values, a third of them
+// for the weights, a fifth for the codes.
 //
 // The range of keys begins at a multiple of a step, so each 16 keys lie in one page: its number is one scalar load (one for the step where pages are as
-// long), made a step ahead of the rows' loads, and the rows have one base.
+// long), made two steps ahead of the rows' use and looked at when the rows are loaded, and the rows have one base.
 //
 // Scores are formed transposed, S^T = K Q^T: a lane then holds scores of one row only, keys 4 (lane / 16) + i of each 16, and the same
 // registers are the operand of O^T = V^T P^T when its keys are counted in that order.  K goes from memory into the operand registers as it
@@ -119,9 +121,10 @@ __device__ __forceinline__ void paged_join(const PagedArgs &a, const int unit, c
     }
 }
 
-// Rows that no other workgroup reads pass by the caches: 32 x 8000 tokens of 8 heads in bf16 186 us, 212 by ordinary loads; one sequence of 131071 in 4
-// bits 30.8, 33.3.  Rows that several tiles read do not (64 heads on one key head, 8 x 32000 in bf16: 64 us so, 52 by ordinary loads), nor rows
-// shorter than half a cache line, whose line is another head's too (24 x 9000 in 4 bits, 64 values a head: 27.8, 25.0).
+// Rows that no other workgroup reads pass by the caches: 32 sequences of 593 to 4096 tokens, 32 key heads of 128 bf16 values 187 us (6.6 TB/s), 212 by
+// ordinary loads; one of 131071 tokens, 8 key heads in 4 bits 31.2, 33.6.  Rows that several tiles read do not (64 heads on one key head,
+// 8 x 32000 tokens in bf16: 64 us so, 52 by ordinary loads), nor rows shorter than half a cache line, whose line is another head's too (24 x 9000
+// tokens in 4 bits, 16 key heads of 64 values, a window of 4096: 27.8, 25.2).
 template <bool ONCE, class T>
 __device__ __forceinline__ T read_row(const T *p)
 {

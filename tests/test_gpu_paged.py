@@ -529,3 +529,49 @@ def test_two_streams_with_contexts_of_their_own(clada):
                 got[i].append(clada.paged_attn(ctxs[i], q, pool.cache, lens[i]))
     torch.cuda.synchronize()
     assert all(torch.equal(x, w) for g, w in zip(got, want) for x in g)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("cap,scale", [(50.0, None), (50.0, -0.1), (2.0, 0.3), (0.01, 0.2), (1e4, 1e-3), (1e-3, 30.0), (7.0, 0.0)])
+def test_capped_prompts(clada, ctx, kind, cap, scale):
+    """A cap alone, on tiles that every row sees: products far below it, around it and far above, scales of both signs and zero."""
+    _case(clada, ctx, kind, 128, 4, 2, 200, [457, 200], page=64, seed=11, cap=cap, scale=scale)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_graphs_and_eager_calls_take_turns_with_one_workspace(clada, kind):
+    """Two captured calls of different sizes, their keys split among workgroups, and an eager one on the same context: whatever the order, each finds the
+    workspace as it needs it."""
+    D, Hq, H, page = 64, 4, 2, 32
+    shapes = [(1, 1, [4999]), (3, 2, [900, 2000, 31]), (2, 40, [700, 1300])]
+    ctx = clada.Context(0, max(clada.attn_workspace_bytes(B, T, Hq, D) for B, T, _ in shapes))
+    rng = np.random.default_rng(8)
+    pool = Pool(clada, kind, 200, H, page, D, np.stack([rng.permutation(200)[:160] for _ in range(3)]), seed=5)
+    qs = [to_dev(rng.standard_normal((B, T, Hq, D)), _np_dtype(kind)) for B, T, _ in shapes]
+    lens, outs = [_ints(n) for _, _, n in shapes], [torch.zeros_like(q) for q in qs]
+
+    def call(i, c, out):
+        return clada.paged_attn(c, qs[i], pool.cache, lens[i], out=out)
+
+    want = []
+    for i, (B, T, _) in enumerate(shapes):
+        alone = clada.Context(0, clada.attn_workspace_bytes(B, T, Hq, D))
+        want.append(call(i, alone, torch.zeros_like(qs[i])))
+        call(i, ctx, outs[i])
+        torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        graphs = []
+        for i in (0, 1):
+            clada.graph_begin(ctx)
+            call(i, ctx, outs[i])
+            graphs.append(clada.graph_end(ctx))
+        for order in ((0, 1, 2), (1, 0, 2), (2, 0, 0, 1), (1, 2, 1, 0)):
+            for out in outs:
+                out.zero_()
+            for i in order:
+                graphs[i].launch() if i < 2 else call(2, ctx, outs[2])
+            torch.cuda.synchronize()
+            assert all(torch.equal(o, w) for o, w in zip(outs, want)), order
+    torch.cuda.synchronize()

@@ -112,3 +112,12 @@ def test_the_binding_takes_tensors_on_the_gpu_alone(b):
     x, t = torch.zeros(4, 2, 16, 64), torch.zeros(1, 4, dtype=torch.int32)
     with pytest.raises(AssertionError):
         b.PagedCache(x, x, t)
+
+
+def test_strides_that_the_kernels_do_not_reach(b):
+    c = Calls(b)
+    for most in (dict(stride_n=1 << 26, stride_h=1 << 31, stride_p=1 << 33), dict(stride_n=1 << 26, heads=1, pages=1)):
+        assert c.read(cache=most) == c.attn(cache=most) == c.append(cache=most) == WORKSPACE
+    for bad in (dict(stride_n=(1 << 26) + 32), dict(stride_p=(1 << 33) + 32), dict(stride_n=1 << 62), dict(stride_p=1 << 62)):
+        assert c.read(cache=bad) == c.attn(cache=bad) == c.append(cache=bad) == SHAPE, bad
+    c.lib.clada_destroy(c.h)
