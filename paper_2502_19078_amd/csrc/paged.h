@@ -196,6 +196,19 @@ __device__ __forceinline__ float2 load_past(const void *from)
     return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const unsigned long long *>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
+// Four values of the partial outputs at once, the same way: `at` counts values from part_o on (fewer than 2^24 of them: splits are made up to two workgroups a compute unit).
+constexpr int PAST_CACHES = 16;                              // the instructions' sc1
+__device__ __forceinline__ void store_past4(float *part_o, unsigned int at, f32x4 v)
+{
+    const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(part_o, 0, -1, 0x00027000);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), all, at * 4, 0, PAST_CACHES);
+}
+__device__ __forceinline__ f32x4 load_past4(float *part_o, unsigned int at)
+{
+    const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(part_o, 0, -1, 0x00027000);
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(all, at * 4, 0, PAST_CACHES));
+}
+
 // What a row of a split, or of a call without splits, leaves behind: by a wave that holds it as above.
 template <int ES>
 __device__ __forceinline__ void paged_store_row(const PagedArgs &a, const RowAgain &r, const RowAt &at, int part)

@@ -68,7 +68,7 @@ __device__ __forceinline__ void paged_join(const PagedArgs &a, const int unit, c
         const int r = min(x + group % pass, R - 1), i = (r0 + r) / a.G;
         const RowAt at = row_at(a, false, b, h, r0 + r, i);
         const float2 *ml = a.part_ml + at.lse * a.splits;
-        const float *po = a.part_o + at.lse * a.splits * a.D + (dim < a.D ? dim : 0);
+        const unsigned int po = (unsigned int)at.lse * a.splits * a.D + (dim < a.D ? dim : 0);
         float m = NEG_INF, l = 0.0f;
         f32x4 o = {0, 0, 0, 0};
         constexpr int N = 4;                                 // loads in flight
@@ -79,8 +79,7 @@ __device__ __forceinline__ void paged_join(const PagedArgs &a, const int unit, c
             for (int j = 0; j < N; ++j) {
                 const int s = min(s0 + j * subs, a.splits - 1);
                 v[j] = load_past(ml + s);
-                const float2 p0 = load_past(po + (int64_t)s * a.D), p1 = load_past(po + (int64_t)s * a.D + 2);
-                part[j] = f32x4{p0.x, p0.y, p1.x, p1.y};
+                part[j] = load_past4(a.part_o, po + (unsigned int)s * a.D);
             }
 #pragma unroll
             for (int j = 0; j < N; ++j) {
@@ -516,13 +515,9 @@ __device__ __forceinline__ void paged_rows(const PagedArgs &a, const int block, 
         if (mine) {
             const int64_t part = at.lse * a.splits + split;
             if (g == 0 && wave == 0) store_past(&a.part_ml[part], make_float2(m, l));
-            float *to = a.part_o + part * Dd;
 #pragma unroll
             for (int x = 0; x < OUT; ++x)
-                if (dim(x) < Dd && k0 < k1) {                // (nothing for a split that has no keys)
-                    store_past(to + dim(x), make_float2(v[x][0], v[x][1]));
-                    store_past(to + dim(x) + 2, make_float2(v[x][2], v[x][3]));
-                }
+                if (dim(x) < Dd && k0 < k1) store_past4(a.part_o, (unsigned int)part * Dd + dim(x), v[x]);      // (nothing for a split that has no keys)
         }
         paged_join<ES, 64 * WAVES>(a, block / a.splits, b, h, r0, min(rows - r0, TILE), lds);
         return;
