@@ -54,9 +54,12 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     a.slopes = scores->slopes;
     const double log2e = 1.4426950408889634;
     a.scale2 = (float)(scores->scale * log2e);
-    if (scores->cap > 0.0f) {
+    // A cap 2^100 scales away is none for products below 2^88 (tanh is its argument there to 2^-24), and its quotient could leave fp32's range; one that
+    // is nothing beside the scale cuts all products but zero, as the largest quotient does.
+    const double quotient = scores->cap > 0.0f ? (double)scores->scale / scores->cap : 0.0;
+    if (scores->cap > 0.0f && scores->cap * log2e < 3e38 && (scores->scale == 0.0f || fabs(quotient) >= 0x1p-100)) {
         a.cap2 = (float)(scores->cap * log2e);
-        a.inv_cap_scale = (float)((double)scores->scale / scores->cap);
+        a.inv_cap_scale = (float)fmax(fmin(quotient, 3e38), -3e38);
         const float ratio = fabsf(a.inv_cap_scale);          // (the polynomial's coefficients hold its ninth power)
         a.cap_limit = ratio >= 0x1p-12f && ratio <= 0x1p12f ? 0.7f / ratio : -1.0f;
     }

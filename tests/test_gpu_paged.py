@@ -575,3 +575,19 @@ def test_graphs_and_eager_calls_take_turns_with_one_workspace(clada, kind):
             torch.cuda.synchronize()
             assert all(torch.equal(o, w) for o, w in zip(outs, want)), order
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("T", [1, 100])
+def test_caps_at_the_ends_of_the_range(clada, ctx, kind, T):
+    """A cap far above every score is none; one far below makes all weights equal."""
+    D, H = 64, 2
+    pool = Pool(clada, kind, 20, H, 16, D, np.arange(20).reshape(1, 20), seed=6)
+    q = to_dev(np.random.default_rng(6).standard_normal((1, T, 4, D)), _np_dtype(kind))
+    want, lse = clada.paged_attn(ctx, q, pool.cache, _ints([300]), want_lse=True)
+    for cap in (3e38, 1e36, 1e33):
+        got = clada.paged_attn(ctx, q, pool.cache, _ints([300]), cap=cap, want_lse=True)
+        assert torch.equal(got[0], want) and torch.equal(got[1], lse), cap
+    for cap in (1e-42, 1e-30):
+        for scale in (None, -3.0):
+            _case(clada, ctx, kind, D, 4, H, T, [300, 37 + T], page=16, seed=7, cap=cap, scale=scale)
