@@ -578,8 +578,8 @@ typedef struct {
  * max_len is what the caller knows about lens, which splits long sequences among workgroups: no entry is above it (more is taken as it); 0: as
  * much as the table has room for.  The workspace is that of clada_attn_workspace_bytes.  Pages that a query does not see do not reach its
  * output, whatever they hold.  The weights of bf16 and 4-bit calls enter the product with v as in clada_window_attn, and a cap's tanh is off by a
- * few 2^-24 of the cap there; a cap of 2^100 |scale| or more is none.  Bit-reproducible from run to run.  A row beside whose own keys a value that is not finite is read for other rows is computed a second time by itself: right, but
- * hundreds of times slower. */
+ * few 2^-24 of the cap there; a cap of 2^100 |scale| or more is none.  Bit-reproducible from run to run.  A row beside whose own keys a value
+ * that is not finite is read for other rows is computed a second time by itself: right, but hundreds of times slower. */
 clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, const clada_paged_cache *cache, const int32_t *lens,
                               const int32_t *q_lens, int32_t B, int32_t T, int32_t Hq, int32_t max_len, const clada_attn_scores *scores,
                               const clada_heads *out, float *lse, void *hip_stream);
