@@ -60,8 +60,11 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     if (scores->cap > 0.0f && scores->cap * log2e < 3e38 && (scores->scale == 0.0f || fabs(quotient) >= 0x1p-100)) {
         a.cap2 = (float)(scores->cap * log2e);
         a.inv_cap_scale = (float)fmax(fmin(quotient, 3e38), -3e38);
-        const float ratio = fabsf(a.inv_cap_scale);          // (the polynomial's coefficients hold its ninth power)
-        a.cap_limit = ratio >= 0x1p-12f && ratio <= 0x1p12f ? 0.7f / ratio : -1.0f;
+        // The polynomial's coefficients are cap2 ratio, cap2 ratio^3 .. cap2 ratio^9 times 1 to 0.013: all of them normal numbers of fp32, or none is
+        // used (an infinite one times a product of zero is no zero).
+        const double ratio = fabs((double)a.inv_cap_scale), c1 = a.cap2 * ratio, c9 = a.cap2 * pow(ratio, 9.0);
+        const bool fits = ratio >= 0x1p-12 && ratio <= 0x1p12 && fmin(c1, c9) >= 0x1p-118 && fmax(c1, c9) <= 0x1p120;
+        a.cap_limit = fits ? 0.7f / fabsf(a.inv_cap_scale) : -1.0f;
     }
     const AttnPath path = T == 1 || T * a.G <= 16 ? ATTN_ROWS : ATTN_TILES;
     const int tile = a.tile_rows = path == ATTN_TILES ? 128 : cache->type != CLADA_PAGE_F32 && T * a.G <= 8 ? 8 : 16;
