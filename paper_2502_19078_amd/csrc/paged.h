@@ -94,9 +94,9 @@ __device__ __forceinline__ float paged_cap_poly(float cap2, float u)
     p = fmaf(p, s, 0.99999850f);
     return u * cap2 * p;
 }
-__device__ __forceinline__ float paged_cap_far(float cap2, float u)
+__device__ __forceinline__ float paged_cap_far(float cap2, float u)      // (halves, so that twice the cap, which fp32 may not hold, is never formed)
 {
-    return fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * 2.8853900817779268f)), cap2);
+    return fmaf(-cap2, __builtin_amdgcn_rcpf(fmaf(0.5f, __builtin_amdgcn_exp2f(u * 2.8853900817779268f), 0.5f)), cap2);
 }
 template <PagedType TY>
 __device__ __forceinline__ float paged_capped(float cap2, float u)
