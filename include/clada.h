@@ -502,7 +502,7 @@ size_t clada_attn_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t d);
  * Query head h reads key head h / (Hq / heads).  A query that sees nothing (a row past q_lens[b], a negative position) gives zeros
  * and an lse of -inf.  T = 1 is a decode step, T = lens a prompt.  Without a ring lens[b] <= capacity (more is taken as capacity);
  * with one, window >= 1, ring >= window + T - 1 and sinks <= n_sink.  Cache rows that a query does not see do not reach its output,
- * whatever they hold.  out must not overlap q.  Scores, sums and outputs are accumulated in fp32 (values whose weighted sum leaves fp32's
+ * whatever they hold.  out must not overlap q; |scale| is at most 2.35e38 (scores are formed in base 2).  Scores, sums and outputs are accumulated in fp32 (values whose weighted sum leaves fp32's
  * range give infinities, also where their mean would not); the weights of bf16 calls enter the product
  * with v as one bf16 (T > 1 and more than 16 rows T Hq / heads) or as two.  Bit-reproducible from run to run.
  * A row beside whose own keys a value that is not finite is read for other rows, and on more than 16 rows one whose scores rise by 94 powers of two or
@@ -565,8 +565,8 @@ clada_status clada_paged_read(clada_ctx *ctx, const clada_paged_cache *cache, co
  *   seen where  p <= pos  or  p < prefix_lens[b] (a prefix that is seen from both sides),
  *   and         p > pos - window  or  window = 0,   and   p >= first[b][t] (the first position of the query's document). */
 typedef struct {
-    float scale;
-    float cap;                              /* 0: none */
+    float scale;                            /* |scale| at most 2.35e38, or a cap */
+    float cap;                              /* 0: none; at most 2.35e38, or none for its scale (see clada_paged_attn) */
     const float *slopes;                    /* device [Hq] or NULL */
     const int32_t *prefix_lens;             /* device [B] or NULL */
     const int32_t *first;                   /* device [B][T] or NULL */

@@ -62,7 +62,7 @@ clada_status check_call(clada_ctx *ctx, const clada_kv_cache *cache, int32_t B, 
     if (Hq < 1 || Hq > CLADA_ATTN_MAX_HEADS || Hq % cache->heads)
         return clada_fail(ctx, CLADA_ERR_SHAPE, "%d query heads: need a multiple of the cache's %d in [1,%d]", Hq, cache->heads, CLADA_ATTN_MAX_HEADS);
     if (cache->batch < B) return clada_fail(ctx, CLADA_ERR_SHAPE, "the cache holds %d sequences, the call has %d", cache->batch, B);
-    if (!isfinite(scale)) return clada_fail(ctx, CLADA_ERR_VALUE, "scale is not finite");
+    if (!isfinite((float)(scale * 1.4426950408889634))) return clada_fail(ctx, CLADA_ERR_VALUE, "scale=%g is not finite, or not in base 2", scale);
     if (((uintptr_t)lens | (uintptr_t)q_lens | (uintptr_t)lse) & 3u) return clada_fail(ctx, CLADA_ERR_ALIGN, "lens, q_lens and lse must be 4-byte aligned");
     return CLADA_OK;
 }

@@ -1,4 +1,5 @@
 // clada_paged_attn: what it accepts, and how a call is cut into workgroups.
+#include <float.h>
 #include <math.h>
 
 #include "paged.h"
@@ -18,6 +19,13 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     if (cache->batch < B) return clada_fail(ctx, CLADA_ERR_SHAPE, "the cache holds %d sequences, the call has %d", cache->batch, B);
     if (!isfinite(scores->scale)) return clada_fail(ctx, CLADA_ERR_VALUE, "scale is not finite");
     if (!(scores->cap >= 0.0f) || !isfinite(scores->cap)) return clada_fail(ctx, CLADA_ERR_VALUE, "cap=%g is negative or not finite", scores->cap);
+    // A cap 2^100 scales away is none for products below 2^88 (tanh is its argument there to 2^-24), and its quotient could leave fp32's range; one that
+    // is nothing beside the scale cuts all products but zero, as the largest quotient does.  What the scores are formed with has to be a number of
+    // fp32 in base 2 too.
+    const double log2e = 1.4426950408889634, quotient = scores->cap > 0.0f ? (double)scores->scale / scores->cap : 0.0;
+    const bool capped = scores->cap > 0.0f && (scores->scale == 0.0f ? scores->cap * log2e <= FLT_MAX : fabs(quotient) >= 0x1p-100);
+    if (fabs((capped ? scores->cap : scores->scale) * log2e) > FLT_MAX)
+        return clada_fail(ctx, CLADA_ERR_VALUE, "scale=%g, cap=%g: scores beyond fp32", scores->scale, scores->cap);
     if (scores->window < 0 || max_len < 0) return clada_fail(ctx, CLADA_ERR_VALUE, "window=%d, max_len=%d: negative", scores->window, max_len);
     if (((uintptr_t)lens | (uintptr_t)q_lens | (uintptr_t)lse | (uintptr_t)scores->slopes | (uintptr_t)scores->prefix_lens | (uintptr_t)scores->first) & 3u)
         return clada_fail(ctx, CLADA_ERR_ALIGN, "lens, q_lens, lse, slopes, prefix_lens and first must be 4-byte aligned");
@@ -52,12 +60,8 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     a.first = scores->first;
     a.prefix_lens = scores->prefix_lens;
     a.slopes = scores->slopes;
-    const double log2e = 1.4426950408889634;
     a.scale2 = (float)(scores->scale * log2e);
-    // A cap 2^100 scales away is none for products below 2^88 (tanh is its argument there to 2^-24), and its quotient could leave fp32's range; one that
-    // is nothing beside the scale cuts all products but zero, as the largest quotient does.
-    const double quotient = scores->cap > 0.0f ? (double)scores->scale / scores->cap : 0.0;
-    if (scores->cap > 0.0f && scores->cap * log2e < 3e38 && (scores->scale == 0.0f || fabs(quotient) >= 0x1p-100)) {
+    if (capped) {
         a.cap2 = (float)(scores->cap * log2e);
         a.inv_cap_scale = (float)fmax(fmin(quotient, 3e38), -3e38);
         // The polynomial's coefficients are cap2 ratio, cap2 ratio^3 .. cap2 ratio^9 times 1 to 0.013: all of them normal numbers of fp32, or none is
