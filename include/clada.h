@@ -529,9 +529,9 @@ clada_status clada_shared_prefix_attn(clada_ctx *ctx, const clada_heads *q, cons
  *
  * CLADA_PAGE_MX4 holds a value in 4 bits (d a multiple of 32): 32 neighbours of a row share a power of two, 2^(byte - 127) with one byte in
  * k_scales / v_scales (byte 255: all 32 are NaN), and a value is 0, 0.5, 1, 1.5, 2, 3, 4 or 6 of it, codes 0 to 7, with 8 added for a
- * minus; the lower of two neighbours lies in the lower half of a byte.  That is 17 bytes for 32 values, each exact in bf16; queries, new
- * rows and outputs are bf16.  k and v have d/2 bytes a row, and the scales lie alike: the byte for the element at offset i of k
- * is k_scales[i / 32].  A block is stored with the power of two 2^(e - 2) where its largest magnitude is in [2^e, 1.75 2^e), twice that above
+ * minus; the lower of two neighbours lies in the lower half of a byte.  That is 17 bytes for 32 values, each exact in bf16
+ * (byte 0 too; under 253 and 254, which no call stores, those of 2^128 and more are infinite); queries, new rows and outputs are bf16.
+ * k and v have d/2 bytes a row, and the scales lie alike: the byte for the element at offset i of k is k_scales[i / 32].  A block is stored with the power of two 2^(e - 2) where its largest magnitude is in [2^e, 1.75 2^e), twice that above
  * (2^-126 at least, 2^125 at most); values go to the nearest code, ties to the even one, 6 the largest.  A block that holds a value that is not finite is stored as NaN. */
 typedef enum { CLADA_PAGE_F32 = 0, CLADA_PAGE_BF16 = 1, CLADA_PAGE_MX4 = 2 } clada_page_type;
 #define CLADA_PAGE_MIN 16

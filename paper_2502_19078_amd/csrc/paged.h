@@ -51,7 +51,7 @@ __device__ __forceinline__ int64_t paged_unit_at(const PagedKV &pg, int page, in
     return (int64_t)((unsigned long long)(unsigned int)page * pg.sp + (unsigned long long)(unsigned int)row * pg.sn);
 }
 
-// 2^(byte - 127); NaN for 255 (what the conversions below make of an infinite scale).
+// What the conversions below take for 2^(byte - 127): they use its exponent alone, so that 0 is 2^-127 too, and 255 (an infinity) gives NaN.
 __device__ __forceinline__ float paged_scale(unsigned int byte) { return __uint_as_float(byte << 23); }
 
 // Eight values of 4 bits (a word) as eight bf16.

@@ -1,4 +1,5 @@
-"""The paged cache's calls at the ends of what they accept: scales and caps near fp32's range, long prompts."""
+"""The paged cache's calls at the ends of what they accept: scales and caps near fp32's range, long prompts,
+every exponent byte of 4-bit pages, wide rows, long pages."""
 import math
 
 import numpy as np
@@ -9,7 +10,7 @@ import attention_ref as ref
 import paged_dense as dense
 import paged_ref as paged
 from gpu_util import DEV, to_dev, to_np
-from test_gpu_paged import TYPES, Pool, _ints, _np_dtype, clada, ctx  # noqa: F401 (fixtures)
+from test_gpu_paged import TYPES, Pool, _case, _ints, _np_dtype, clada, ctx  # noqa: F401 (fixtures)
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +115,89 @@ def test_steady_tiles(clada, ctx, kind, D, mods):
                                 slopes=None if slopes is None else torch.from_numpy(slopes).to(DEV))
     r = dense.paged_attn(to_np(q), pool.held("k"), pool.held("v"), order, STEADY["page"], n, scale, window, cap, slopes, fp32=kind == "f32")
     ref.check(to_np(out), to_np(lse), r, _np_dtype(kind), weights_bf16=True)
+
+
+# ------------------------------------------------------------------------------------------------ every exponent byte
+def _every_byte(clada, table):
+    """A pool of 16 pages of 16 rows, one head of 64 values: row b has the byte b and all 16 codes twice, then 255 - b and the codes backwards."""
+    pool = Pool(clada, "mx4", 16, 1, 16, 64, table, seed=1)
+    byte = np.stack([np.arange(256), 255 - np.arange(256)], -1)
+    code = np.tile(np.concatenate([np.arange(32) % 16, 15 - np.arange(32) % 16]), (256, 1))
+    want = paged.values(code, byte)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)      # beyond bf16
+    for n in "kv":
+        pool.t[n].copy_(torch.from_numpy(paged.pack(code).reshape(16, 1, 16, 32)))
+        pool.t[n + "s"].copy_(torch.from_numpy(byte.astype(np.uint8).reshape(16, 1, 16, 2)))
+    return pool, want
+
+
+def test_every_byte_is_read(clada, ctx):
+    """2^(byte - 127) from 0 on: values below the normal numbers are exact, those from 2^128 on infinite, and 255 is NaN for every code."""
+    pool, want = _every_byte(clada, [list(range(16))])
+    for x in clada.paged_read(ctx, pool.cache, _ints([list(range(256))])):
+        got = to_np(x)[0, :, 0]
+        bad = ~((got == want) | (np.isnan(got) & np.isnan(want)))
+        assert not bad.any(), [(b, got[b][bad[b]][:4], want[b][bad[b]][:4]) for b in np.nonzero(bad.any(-1))[0][:4]]
+
+
+@pytest.mark.parametrize("T", [1, 7, 40, 256])
+def test_every_byte_as_a_value(clada, ctx, T):
+    """A window of one: each query's output is the value that it sees, to the products' and the output's handling of numbers below 2^-126."""
+    pool, want = _every_byte(clada, [list(range(16))])
+    pool.t["k"].zero_()
+    pool.t["ks"].fill_(127)
+    q = to_dev(np.random.default_rng(2).standard_normal((1, T, 1, 64)), "bf16")
+    for n in sorted({256, 255, 200, T}):
+        if n < T:
+            continue
+        got, w = to_np(clada.paged_attn(ctx, q, pool.cache, _ints([n]), window=1))[0, :, 0], want[n - T:n]
+        assert np.array_equal(np.isnan(got), np.isnan(w)), n
+        near = np.abs(np.where(np.isfinite(w), got, 0.0) - np.where(np.isfinite(w), w, 0.0)) <= 2.0 ** -126
+        assert np.all((got == w) | np.isnan(w) | (near & (np.abs(w) <= 2.0 ** -126))), n
+
+
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("byte,most,q", [(0, 7, 2.0 ** 126), (1, 7, 2.0 ** 125), (252, 7, 2.0 ** -126), (253, 5, 2.0 ** -126), (254, 3, 2.0 ** -126)])
+def test_keys_at_both_ends_of_the_bytes(clada, ctx, byte, most, q, T):
+    """Keys of the smallest and the largest powers of two, times queries that bring the scores back to units."""
+    D, n = 64, T + 60
+    pool = Pool(clada, "mx4", 8, 1, 16, D, [list(range(8))], seed=5)
+    rng = np.random.default_rng(6)
+    code = rng.integers(0, most + 1, (8, 1, 16, D)) + 8 * rng.integers(0, 2, (8, 1, 16, D))
+    pool.t["k"].copy_(torch.from_numpy(paged.pack(code)))
+    pool.t["ks"].fill_(byte)
+    qs = to_dev(q * rng.choice([-1.0, 0.0, 0.0, 1.0], (1, T, 2, D)), "bf16")
+    out, lse = clada.paged_attn(ctx, qs, pool.cache, _ints([n]), scale=0.5, want_lse=True)
+    r = paged.paged_attn(to_np(qs), pool.held("k"), pool.held("v"), [list(range(8))], 16, [n], [T], 0.5)
+    ref.check(to_np(out), to_np(lse), r, "bf16", weights_bf16=T > 1)
+
+
+# ------------------------------------------------------------------------------------------------ sizes
+@pytest.mark.parametrize("Hq,H", [(1, 1), (6, 2), (20, 1), (40, 1)])
+def test_4_bit_heads_of_224(clada, ctx, Hq, H):
+    """Seven blocks a row: a quarter of it, which a lane group takes, touches three of their exponents."""
+    _case(clada, ctx, "mx4", 224, Hq, H, 1, [1, 0, 37, 300, 129], page=16, seed=Hq)
+    _case(clada, ctx, "mx4", 224, Hq, H, 1, [300, 40, 33], page=64, seed=Hq + 1, heads_last=True, window=32, cap=3.0, bias=0.3)
+    _case(clada, ctx, "mx4", 224, Hq, H, 9, [70, 9, 8], [9, 9, 8], page=16, seed=Hq + 2)
+    _case(clada, ctx, "mx4", 224, Hq, H, 130, [207, 65], [130, 65], page=32, seed=Hq + 3, window=50, cap=4.0, bias=0.2)
+
+
+@pytest.mark.parametrize("D", [160, 192, 224])
+@pytest.mark.parametrize("page,heads_last", [(16, False), (256, True)])
+def test_wide_4_bit_rows_are_read(clada, ctx, D, page, heads_last):
+    pool = Pool(clada, "mx4", 3, 2, page, D, [[2, 0, -1]], seed=D, heads_last=heads_last)
+    pos = [0, page - 1, page, 2 * page - 1, 2 * page, -1, 5]
+    k, v = clada.paged_read(ctx, pool.cache, _ints([pos]))
+    for got, n in ((k, "k"), (v, "v")):
+        for t, p in enumerate(pos):
+            want = pool.held(n)[[2, 0][p // page], :, p % page] if 0 <= p < 2 * page else np.zeros((2, D))
+            assert np.array_equal(to_np(got)[0, t], want), (n, p)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("page", [256, 4096])
+@pytest.mark.parametrize("T", [1, 7, 70])
+def test_long_pages(clada, ctx, kind, page, T):
+    """Pages of more rows than a tile, up to the longest: lengths that end on their border, one row around it and inside them."""
+    _case(clada, ctx, kind, 32, 2, 1, T, [page + T, page, page + 1, 2 * page + 77], [T, T, min(T, 1), T], page=page, seed=T, cap=5.0)
+    _case(clada, ctx, kind, 32, 2, 1, T, [2 * page + 5, page + 3], page=page, seed=T + 1, window=300, heads_last=True, holes=[(0, 1)])
