@@ -15,7 +15,8 @@
  *     nothing: scratch lives in the context's workspace, sized at
  *     clada_create() with clada_workspace_bytes().
  *   - A context serves one stream at a time; calls issued to one context from
- *     several threads or streams at once race on its workspace.
+ *     several threads or streams at once race on its workspace, and may leave counters
+ *     there that spoil later calls: destroy such a context.
  *   - Every call returns a clada_status and never throws or aborts;
  *     clada_last_error() gives the text of the last failure of that context.
  *   - Weights are neuron-major: W_gate[d_ff][d], W_up[d_ff][d], W_down[d_ff][d],
