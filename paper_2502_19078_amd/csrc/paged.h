@@ -84,6 +84,8 @@ __device__ __forceinline__ RowSpan paged_span(const PagedArgs &a, int b, int t, 
 // cap log2(e) tanh(u), u = x / cap.  In 16 and 4 bits: up to |u| = 0.7 an odd polynomial of five terms (least largest error, 1.6 2^-24, found by
 // weighted least squares; seven instructions of a clock each in place of three and two that take four), beyond it 1 - 2 / (1 + exp(2 u)).  Both are off
 // by a few 2^-24 of cap; in fp32 calls, whose scores may be small beside it, tanhf is not.
+// In units of 2^-24 cap, |u| <= 0.7: the argument's two roundings 0.9 (u / cosh^2 u <= 0.45), the polynomial 1.6, its steps 1, the products and cap2 1.8: below
+// 6.  With the scale in the coefficients (paged_tiles.h), each k-th power's off by 2 k + 3 at most: 4.9, the polynomial 1.6, its steps 1.1: below 8.
 constexpr float PAGED_CAP_POLY = 0.7f;
 __device__ __forceinline__ float paged_cap_poly(float cap2, float u)
 {

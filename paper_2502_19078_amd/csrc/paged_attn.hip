@@ -82,7 +82,7 @@ extern "C" clada_status clada_paged_attn(clada_ctx *ctx, const clada_heads *q, c
     const bool eight_waves = cache->type == CLADA_PAGE_MX4 && cache->d <= 128;
     a.splits = clada_attn_splits(units, keys, path == ATTN_ROWS && (eight_waves || cache->d >= 128) ? ctx->num_cu : 2 * ctx->num_cu);
     a.snake = path == ATTN_TILES && units * a.splits <= 2 * ctx->num_cu;
-    if (units > PAGED_MAX_ARRIVED) a.splits = 1;
+    if (units > PAGED_MAX_ARRIVED) a.splits = 1;             // (there is a counter for each; 512 units are one split each already)
     a.arrived = (int *)(ctx->ws + PAGED_ARRIVED);
     if (a.splits > 1 && (st = clada_attn_place(ctx, a)) != CLADA_OK) return st;
     const auto launch = cache->type == CLADA_PAGE_MX4 ? clada_paged_launch_mx4 : cache->type == CLADA_PAGE_BF16 ? clada_paged_launch_bf16 : clada_paged_launch_f32;

@@ -6,7 +6,7 @@
 // Bound by the pages' bytes (HBM): a key head's rows are read once for all query heads of its group.  A workgroup takes a tile of 8 or 16 rows and
 // one split of their keys; its four waves (eight for rows of 4 bits) take steps of 16 or 32 keys in turn, each with a running softmax of its
 // own, so nothing waits inside the loop; the waves' results are joined through LDS, those of the splits by the last workgroup to arrive.
-// Rows of 4 bits come at 3.4 to 4.6 TB/s: half of a wave's time is a wait for the step on its way, and the vector units are busy for 40 to 55 % (about 160
+// Rows of 4 bits come at 2.9 to 4.6 TB/s: 41 to 47 % of a wave's time is a wait for the step on its way, and the vector units are busy for 43 to 52 % of the busy cycles (about 160
 // instructions for 32 keys of 64 values).  Two steps on their way, or each weight formed once for tiles of 4 rows (a third fewer
 // instructions), changed the time by less than 3 %; twice the workgroups cost 6 us, the time in which the last one reads the others' results.
 //
@@ -121,10 +121,12 @@ __device__ __forceinline__ void paged_join(const PagedArgs &a, const int unit, c
     }
 }
 
-// Rows that no other workgroup reads pass by the caches: 32 sequences of 593 to 4096 tokens, 32 key heads of 128 bf16 values 187 us (6.6 TB/s), 212 by
+// Rows that one tile of their sequence alone reads pass by the caches: 32 sequences of 593 to 4096 tokens, 32 key heads of 128 bf16 values 187 us (6.6 TB/s), 212 by
 // ordinary loads; one of 131071 tokens, 8 key heads in 4 bits 31.2, 33.6.  Rows that several tiles read do not (64 heads on one key head,
 // 8 x 32000 tokens in bf16: 64 us so, 52 by ordinary loads), nor rows shorter than half a cache line, whose line is another head's too (24 x 9000
 // tokens in 4 bits, 16 key heads of 64 values, a window of 4096: 27.8, 25.2).
+// Sequences that share their pages read the same rows all the same, and lose by it: 32 over one set of 4000 positions, 8 key heads of bf16 44.2 us, 39.4 by
+// ordinary loads, 32 key heads 220 and 143, in 4 bits both 23.2 (80.3 and 90.7 with pages of their own).  The tables, which say so, are on the device.
 template <bool ONCE, class T>
 __device__ __forceinline__ T read_row(const T *p)
 {

@@ -8,15 +8,17 @@
 //
 // Scores are formed transposed (S^T = K Q^T): a lane holds scores of one row only, keys 8 (i / 4) + 4 (lane / 32) + i % 4 of each 32, and the same
 // registers are the second operand of O^T = V^T P^T when its keys are counted in that order (16-bit V is turned by ds_read_tr16).  Weights are
-// rounded to bf16 there (2^-8 at most, to nearest: the size of the output's own rounding); their sum is taken before it.
+// rounded to bf16 there (2^-8 at most, to nearest: the size of the output's own rounding); their sum is taken before it.  Outputs are 0.0021 to 0.0023 off then,
+// 0.0016 by two bf16 a weight, which take the three cases below to 726, 219 and 184 us.
 //
 // Every row sees an interval of keys, so a tile is looked at key by key only where an interval begins or ends, or a page is missing.  Tiles are taken
 // from the last one down: a row's own key, and with a slope the least of its bias, comes first, so that its maximum is set once and a
 // steady loop without a scaling of the sums does for the rest (one inside the loop costs a second set of registers for all of them).
 //
-// Bound by the matrix units and the clock that they leave: 8192 tokens of 5 documents, 32 heads on 8 of 128 bf16 values, capped: 180 us, 0.61 PFLOP/s
-// of useful pairs; 2 x 512 tokens behind 8000 and 6766 in 4 bits 146 us, 0.82; 1000 and 737 tokens of 32 fp32 heads of 80: 152 us, 58 TFLOP/s, the
-// matrix units busy for two thirds of it, a sixth of that for the padding of 80 to 96.  Scores of the next tile between the products of this one need
+// Bound by the matrix and vector units in turn and the clock that they leave (of 2.4 GHz): 8192 tokens, 32 heads on 8 of 128 bf16 values: 556 us, 0.99 PFLOP/s,
+// matrix units 49 %, vector units 43 % of the cycles, at 1.80 GHz; of 5 documents, capped: 183 us, 0.60 PFLOP/s of useful pairs, 26 and 49 % at 2.08; 2 x 512
+// tokens behind 8000 and 6766 in 4 bits 148 us, 0.81, 35 and 37 % at 2.19.  1000 and 737 tokens of 32 fp32 heads of 80: 152 us, 58 TFLOP/s, the compute units
+// busy for 66 % of it (equal tiles, unequal lengths), the matrix units for 42 %, a sixth of that for the padding of 80 to 96.  Scores of the next tile between the products of this one need
 // twice the registers: spilled at two waves a SIMD (chunk 249 us), 192 us at one; 64 rows a wave 185.
 #pragma once
 #include <type_traits>
@@ -199,7 +201,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs &a, const int id, ch
     };
     // (threads without a chunk write into the padding of a row of K and no V; 4 bits: threads without a row write nothing)
     // The 16-byte chunks of each 64 bytes of a row of bf16 V change places by the row, so that neither the reads nor the writes of four rows meet in a
-    // bank (no conflicts are counted then, 7 million in a chunk of 2 x 512 tokens behind 8000 without; under 1 % of the time, and free).
+    // bank (with bf16 pages no conflicts are counted then; in 4 bits, where a thread writes 64 bytes of a row, 7 million cycles in the chunk).
     const unsigned int put_at = FOUR ? col * 64 : min(col, DP * ES), turn = ES == 2 ? (first_key & 3) * 16 : 0;
     const unsigned int put_k = first_key * KP + put_at, put_v = KT * KP + first_key * VP + (FOUR ? put_at : put_at ^ turn);
     auto put_one = [&](int buf, int q) {                     // write q into LDS

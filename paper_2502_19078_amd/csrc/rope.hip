@@ -3,9 +3,10 @@
 // Every value is read once and written once (HBM): a row (one head of one token) lies on a group of lanes, two 16-byte chunks each; the group
 // sums the squares for the norm, and the value that a rotation pairs with lies in the same chunk (neighbouring pairs) or in the same
 // lane (halves: a lane holds the two chunks that face each other).  A group takes several heads of its token, so the angles and the
-// norm's weights are taken once for them.  4096 tokens of 32 + 8 + 8 heads of 128 bf16 values with norms: 24 us, 4.3 TB/s (44 with
-// a chunk a lane, every angle twice and weights value by value); 1949 tokens of 96 fp32 heads of 80: 30 us, 4.1.
-// Into pages of 4 bits those 4096 tokens take 24 us too: a quarter of the bytes stored for k and v, but by stores of 4 bytes.
+// norm's weights are taken once for them.  4096 tokens of 32 + 8 + 8 heads of 128 bf16 values with norms, one input
+// time and again, which the last-level cache holds: 24 us (44 with a chunk a lane, every angle twice and weights value by value); inputs in turn, into pages:
+// 33 us, 3.1 TB/s, and 1998 tokens of 96 fp32 heads of 80 33 us, 3.9.  Into pages of 4 bits those 4096 tokens take 31 us: a quarter of the bytes
+// stored for k and v, but by stores of 4 bytes.
 //
 // The angle of pair i at position p is p * f_i.  In fp32 that product is off by 2^-24 p f_i radians: at position 100 000 more than a bf16
 // value's rounding.  f_i is therefore held as a 64-bit fraction of a turn, and the integer product wraps whole turns away exactly.
@@ -61,8 +62,9 @@ __device__ __forceinline__ unsigned int quad_move(unsigned int v) { return __flo
 // A rotated value is r (x_i w_i cos + x_j w_j (+-sin)), j its partner and r the norm's factor: two coefficients for every value of a lane,
 // the same for all query heads of a token, and for all key heads.
 // LG lanes a row, two 16-byte chunks each.  FACE (halves, R/2 whole chunks): the two that turn into each other, so that each angle is
-// computed once; otherwise neighbours.  PAIRS: neighbouring values turn together.  Neither: halves that begin inside a chunk; partners
-// are loaded one by one (4096 tokens of 32 + 8 + 8 heads of 128 bf16 values of which 24 turn: 46 us, 22 where 32 do).
+// computed once; otherwise neighbours.  PAIRS: neighbouring values turn together.  Neither: halves that begin inside a chunk, and in 4 bits
+// those that are not whole blocks of 32, whose maximum is found over neighbouring lanes; partners are loaded one by one (4096 tokens of 32 + 8 + 8 heads of 128
+// bf16 values of which 24 turn: 46 us, 22 where 32 do, one input; in 4 bits 32 of 128, or 96 of 96: 68, inputs in turn, 31 where all 128 do).
 template <int ES, int LG, bool PAIRS, bool FACE, RopeInto INTO>
 __global__ void __launch_bounds__(256)
 k_qk_rope(const RopeArgs a)
